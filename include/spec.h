@@ -339,6 +339,72 @@ int spec_sample_accept(void *hip_stream, const float *d_target_logits, const flo
 int spec_set_sampling(spec_ctx *ctx, float temperature, const float *d_uniforms, float *d_target_logits,
                       float *d_draft_logits);
 
+/* Operators for a caller that runs the target model itself over a paged cache: what its verification pass needs between
+   the products, beside the acceptance rules above.  None needs a context; all enqueue on hip_stream (NULL = the default
+   stream) and return without waiting; lengths, pages and rows are read on the device, so a call can be captured into a
+   graph and replayed with other contents.  Rejected proposals need no call: the next round's lengths leave them out and
+   its rows overwrite them (Sec. 3.1).
+
+   spec_paged_cache: the keys and values of one layer in pages of page_size positions (a power of two, 8 to 1024), any
+   number of sequences sharing one pool.  Element i of position p of key head h in page g lies at
+   d_k[g * page_stride + p * pos_stride + h * head_stride + i], values likewise in d_v; strides in elements.  So
+   [n_pages][page_size][n_kv_heads][head_dim] and [n_pages][n_kv_heads][page_size][head_dim] both fit, as does a pool that
+   interleaves keys and values.  head_dim is 64 or 128 (SPEC_ERR_UNSUPPORTED otherwise); d_k and d_v are 16-byte aligned
+   and the strides are multiples of 16 bytes.
+
+   spec_paged_batch: what a pass works on.  Sequence b brings n_b new rows, rows d_row_start[b] .. d_row_start[b + 1] - 1
+   of the row-wise tensors (d_row_start NULL: every sequence brings rows / B); d_len[b] is its cached length, the new rows
+   included, so row i of it is position d_len[b] - n_b + i.  Rows at negative positions are dead (a padded batch), rows
+   behind the last sequence belong to none.  Position p lies in page d_pages[b * pages_stride + p / page_size]; an entry
+   outside [0, n_pages) is an absent page: nothing is written to it and no row sees its positions.  max_rows and max_len
+   are the host's bounds of n_b and d_len[b]: grids and workspaces follow them, what lies beyond is not processed
+   (n_b counts as max_rows, d_len[b] as max_len). */
+typedef struct {
+  int32_t dtype;                             /* SPEC_DTYPE_*: of the cache and of every row-wise tensor */
+  int32_t head_dim, n_kv_heads, page_size, n_pages;
+  int64_t page_stride, pos_stride, head_stride; /* elements */
+  void *d_k, *d_v;
+} spec_paged_cache;
+
+typedef struct {
+  int32_t B, rows;             /* sequences; rows of the row-wise tensors                          */
+  int32_t max_rows, max_len;   /* bounds of n_b (<= rows) and of d_len (<= pages_stride * page_size) */
+  const int32_t *d_row_start;  /* [B + 1] or NULL                                                  */
+  const int32_t *d_len;        /* [B]                                                              */
+  const int32_t *d_pages;      /* [B][pages_stride]                                                */
+  int32_t pages_stride;
+} spec_paged_batch;
+
+/* Appends keys and values to the cache, with the rotary embedding applied on the way (rotate-half pairing, element i of
+   a head with i + rope_dim / 2, as the models above): row i's q and k are turned by the angles p * d_inv_freq[i], p its
+   position, computed in 64 bits; products in fp32, one rounding.  rope_dim: the first elements of a head that turn, a
+   multiple of 16 up to head_dim, 0 for none (learned positions; d_inv_freq may be NULL then).  d_inv_freq: rope_dim / 2
+   doubles, radians a position (theta^(-2i / rope_dim), or scaled as the caller's model wants them).
+     d_q [rows][n_q_heads][head_dim], d_k, d_v [rows][n_kv_heads][head_dim]: row strides in elements, heads dense, so the
+     three may be parts of one product's rows; d_q_out likewise, may be d_q itself (same stride).  n_q_heads = 0: keys and values
+     only, d_q and d_q_out are not looked at.
+   Rows that no sequence owns and dead rows are not written anywhere.  Pointers 16-byte aligned, strides multiples of 16
+   bytes.  Two rows that the pages send to the same place leave one of their values there.                       */
+int spec_paged_append(void *hip_stream, const spec_paged_cache *cache, const spec_paged_batch *batch, int32_t n_q_heads,
+                      const void *d_q, int64_t q_stride, const void *d_k, int64_t k_stride, const void *d_v, int64_t v_stride,
+                      const double *d_inv_freq, int32_t rope_dim, void *d_q_out, int64_t q_out_stride);
+
+/* Attention of every row over its sequence's pages, causal: row at position p sees positions max(0, p - window + 1) .. p
+   (window = 0: from 0 on).  Query head h reads key head h / (n_q_heads / n_kv_heads).  out = sum of softmax(scale * q.k)
+   times v; a row that sees nothing is zeros, and what lies at positions that a row does not see never reaches it, be it
+   infinite or NaN.  Scores, softmax and sums are fp32; softmax weights of 16-bit runs are rounded to the type once for the product
+   with the values.  n_q_heads a multiple of n_kv_heads; scale > 0.
+     d_q, d_out [rows][n_q_heads][head_dim], row strides in elements (alignment as above); rows that no sequence owns are
+     left as they were in d_out.
+     d_workspace: device scratch, 256-byte aligned, at least spec_paged_attention_workspace_bytes(); contents before and
+     after are of no meaning; calls that may overlap need one each.
+   Results do not depend on what other sequences share the pass beyond the order of fp32 sums.                    */
+int spec_paged_attention_workspace_bytes(const spec_paged_cache *cache, const spec_paged_batch *batch, int32_t n_q_heads,
+                                         size_t *bytes);
+int spec_paged_attention(void *hip_stream, const spec_paged_cache *cache, const spec_paged_batch *batch, int32_t n_q_heads,
+                         const void *d_q, int64_t q_stride, float scale, int32_t window, void *d_workspace,
+                         size_t workspace_bytes, void *d_out, int64_t out_stride);
+
 /* Parity aids for the draft step (the call speculate(S, kv_SSM, s) of Alg. 1).
    spec_set_draft_logits: if d_logits is not NULL, every following spec_draft_step also writes the draft
    model's logits behind t_j -- the logits of the last token each sequence fed in -- as fp32 [B][vocab]

@@ -32,7 +32,8 @@ EXPORTS = ["spec_last_error", "spec_workspace_bytes", "spec_init", "spec_destroy
            "spec_read_kernel_timing", "spec_set_hidden_dump", "spec_set_attention_shape", "spec_measure_peaks",
            "spec_set_draft_logits", "spec_read_proposals", "spec_greedy_accept_workspace_bytes", "spec_greedy_accept",
            "spec_greedy_accept_noalloc", "spec_set_gemm_tuning", "spec_read_saturation", "spec_sample_tokens",
-           "spec_sample_accept", "spec_set_sampling"]
+           "spec_sample_accept", "spec_set_sampling", "spec_paged_append", "spec_paged_attention_workspace_bytes",
+           "spec_paged_attention"]
 KCLASS_NAMES = ["gemm_qkv", "gemm_o", "gemm_ffn_in", "gemm_ffn_out", "gemm_head", "attention", "norm", "other",
                 "draft_pass"]
 
@@ -51,6 +52,16 @@ class Weights(C.Structure):
 class RunDesc(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("B_max", C.c_int32), ("s_max", C.c_int32), ("L_max", C.c_int32),
                 ("gen_max", C.c_int32), ("eos_id", C.c_int32), ("proposal_mode", C.c_int32)]
+
+
+class PagedCacheDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("head_dim", C.c_int32), ("n_kv_heads", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32),
+                ("page_stride", C.c_int64), ("pos_stride", C.c_int64), ("head_stride", C.c_int64), ("d_k", C.c_void_p), ("d_v", C.c_void_p)]
+
+
+class PagedBatchDesc(C.Structure):
+    _fields_ = [("B", C.c_int32), ("rows", C.c_int32), ("max_rows", C.c_int32), ("max_len", C.c_int32), ("d_row_start", C.c_void_p),
+                ("d_len", C.c_void_p), ("d_pages", C.c_void_p), ("pages_stride", C.c_int32)]
 
 
 _vp, _i32, _i32p, _f32p, _i64p = C.c_void_p, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_float), C.POINTER(C.c_int64)
@@ -90,6 +101,12 @@ lib.spec_greedy_accept_noalloc.argtypes = [_vp, _vp, _vp, _i32, _i32, _i32, _vp,
 lib.spec_sample_tokens.argtypes = [_vp, _vp, _i32, _i32, C.c_float, _vp, _vp]
 lib.spec_sample_accept.argtypes = [_vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, C.c_float, _vp, _vp, _vp]
 lib.spec_set_sampling.argtypes = [_vp, C.c_float, _vp, _vp, _vp]
+_i64 = C.c_int64
+lib.spec_paged_append.argtypes = [_vp, C.POINTER(PagedCacheDesc), C.POINTER(PagedBatchDesc), _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i32,
+                                  _vp, _i64]
+lib.spec_paged_attention_workspace_bytes.argtypes = [C.POINTER(PagedCacheDesc), C.POINTER(PagedBatchDesc), _i32, C.POINTER(C.c_size_t)]
+lib.spec_paged_attention.argtypes = [_vp, C.POINTER(PagedCacheDesc), C.POINTER(PagedBatchDesc), _i32, _vp, _i64, C.c_float, _i32, _vp, C.c_size_t,
+                                     _vp, _i64]
 lib.spec_set_attention_shape.argtypes = [_vp, _i32]
 lib.spec_set_gemm_tuning.argtypes = [_vp, _i32, _i32, _i32]
 lib.spec_kernel_timing.argtypes = [_vp, _i32]
@@ -218,6 +235,107 @@ def spec_sample_accept(target_logits, draft_logits, proposals, uniforms, tempera
           proposals.data_ptr() if s else None, uniforms.data_ptr(), nB, s, V, float(temperature), chosen.data_ptr(), accepted.data_ptr(),
           emitted.data_ptr())
     return chosen, accepted, emitted
+
+
+_DTYPE_OF = {v: k for k, v in TORCH_DTYPE.items()}
+
+
+class PagedCache:
+    """The keys and values of one layer in pages: k, v [n_pages][page_size][n_kv_heads][head_dim] device tensors of one dtype and one
+    set of strides (any order in memory whose last dimension is dense: a view of [n_pages][n_kv_heads][page_size][head_dim] does)."""
+
+    def __init__(self, k, v):
+        assert k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.device == v.device and k.dtype in _DTYPE_OF
+        assert k.stride() == v.stride() and k.stride(3) == 1
+        self.k, self.v, self.device = k, v, k.device  # the tensors must outlive their use
+        n, size, heads, hd = k.shape
+        self.desc = PagedCacheDesc(_DTYPE_OF[k.dtype], hd, heads, size, n, k.stride(0), k.stride(1), k.stride(2), k.data_ptr(), v.data_ptr())
+
+
+class PagedBatch:
+    """What a pass over a paged cache works on: pages [B][n] int32, lengths [B] int32 (cached positions, the new rows included), rows
+    in all; row_start [B + 1] int32, or None: rows / B of every sequence.  Device tensors, read when a call runs: a program may update
+    them in place between calls.  max_rows, max_len: bounds of a sequence's rows and length (default: what rows and pages allow)."""
+
+    def __init__(self, pages, lengths, rows, row_start=None, max_rows=None, max_len=None):
+        nB = lengths.shape[0]
+        assert pages.dim() == 2 and pages.shape[0] == nB and pages.dtype == torch.int32 and (pages.shape[1] < 2 or pages.stride(1) == 1)
+        assert lengths.dim() == 1 and lengths.dtype == torch.int32 and lengths.is_contiguous()
+        assert row_start is None or (row_start.dtype == torch.int32 and row_start.shape == (nB + 1,) and row_start.is_contiguous())
+        self.pages, self.lengths, self.row_start = pages, lengths, row_start  # must outlive their use
+        self.rows, self.max_rows, self.max_len = rows, max_rows, max_len
+        stride = pages.stride(0) if nB > 1 else pages.shape[1]
+        if max_rows is None:
+            max_rows = rows if row_start is not None else max(1, rows // max(1, nB))
+        self.desc = PagedBatchDesc(nB, rows, max_rows, max_len or 0, None if row_start is None else row_start.data_ptr(), lengths.data_ptr(),
+                                   pages.data_ptr(), stride)
+
+    def _for(self, cache):
+        if self.max_len is None:
+            self.desc.max_len = self.pages.shape[1] * cache.desc.page_size
+        else:
+            assert self.max_len <= self.pages.shape[1] * cache.desc.page_size
+        return C.byref(self.desc)
+
+
+def _heads(t, rows, hd, cache):
+    assert t.dim() == 3 and t.shape[0] == rows and t.shape[2] == hd and _DTYPE_OF.get(t.dtype) == cache.desc.dtype and t.device == cache.device
+    assert t.stride(2) == 1 and (t.shape[1] < 2 or t.stride(1) == hd)
+    return t.data_ptr(), (t.stride(0) if rows > 1 else t.shape[1] * hd)
+
+
+def spec_rope_frequencies(theta, rope_dim, device="cuda:0"):
+    """theta^(-2i / rope_dim), i < rope_dim / 2, as the doubles spec_paged_append takes."""
+    return (float(theta) ** (-torch.arange(0, rope_dim, 2, dtype=torch.float64) / rope_dim)).to(device)
+
+
+def spec_paged_append(cache, batch, q, k, v, inv_freq=None, out=None):
+    """k, v [rows][n_kv_heads][head_dim] into the pages; q [rows][n_q_heads][head_dim] (None: keys and values only) and k rotated by
+    position * inv_freq (float64 [rope_dim / 2], None: no rotation).  -> out, the rotated q (may be q itself); None without q."""
+    d = cache.desc
+    rows = batch.rows
+    kp, ks = _heads(k, rows, d.head_dim, cache)
+    vp, vs = _heads(v, rows, d.head_dim, cache)
+    assert k.shape[1] == v.shape[1] == d.n_kv_heads
+    qp = op = None
+    qs = os_ = nq = 0
+    if q is not None:
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        assert out.shape == q.shape
+        nq = q.shape[1]
+        qp, qs = _heads(q, rows, d.head_dim, cache)
+        op, os_ = _heads(out, rows, d.head_dim, cache)
+    rope = 0
+    if inv_freq is not None:
+        assert inv_freq.dtype == torch.float64 and inv_freq.dim() == 1 and inv_freq.is_contiguous() and inv_freq.device == cache.device
+        rope = 2 * inv_freq.shape[0]
+    _call(cache.device, lib.spec_paged_append, C.byref(d), batch._for(cache), nq, qp, qs, kp, ks, vp, vs,
+          inv_freq.data_ptr() if rope else None, rope, op, os_)
+    return out if q is not None else None
+
+
+def spec_paged_attention_workspace_bytes(cache, batch, n_q_heads):
+    n = C.c_size_t(0)
+    _check(lib.spec_paged_attention_workspace_bytes(C.byref(cache.desc), batch._for(cache), n_q_heads, C.byref(n)))
+    return n.value
+
+
+def spec_paged_attention(cache, batch, q, scale=None, window=0, out=None, workspace=None):
+    """q [rows][n_q_heads][head_dim] over the pages -> out, the same shape.  scale: 1 / sqrt(head_dim) if None.  workspace: a uint8
+    tensor of spec_paged_attention_workspace_bytes() (allocated if None)."""
+    d = cache.desc
+    rows, nq = batch.rows, q.shape[1]
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    assert out.shape == q.shape
+    qp, qs = _heads(q, rows, d.head_dim, cache)
+    op, os_ = _heads(out, rows, d.head_dim, cache)
+    if workspace is None:
+        workspace = torch.empty(spec_paged_attention_workspace_bytes(cache, batch, nq), dtype=torch.uint8, device=q.device)
+    _call(cache.device, lib.spec_paged_attention, C.byref(d), batch._for(cache), nq, qp, qs, d.head_dim ** -0.5 if scale is None else float(scale),
+          int(window), workspace.data_ptr() if workspace.numel() else None, workspace.numel(), op, os_)
+    return out
 
 
 def spec_workspace_bytes(tgt_desc, drf_desc, run):
