@@ -12,17 +12,17 @@ def B():
     return binding
 
 
-def cache(B, **kw):
-    d = dict(dtype=B.DTYPE_BF16, head_dim=128, n_kv_heads=2, page_size=16, n_pages=10, page_stride=16 * 2 * 128, pos_stride=2 * 128, head_stride=128,
+def cache(lib, **kw):
+    d = dict(dtype=lib.DTYPE_BF16, head_dim=128, n_kv_heads=2, page_size=16, n_pages=10, page_stride=16 * 2 * 128, pos_stride=2 * 128, head_stride=128,
              d_k=FAKE, d_v=FAKE)
     d.update(kw)
-    return B.PagedCacheDesc(**d)
+    return lib.PagedCacheDesc(**d)
 
 
-def batch(B, **kw):
+def batch(lib, **kw):
     d = dict(B=2, rows=6, max_rows=3, max_len=160, d_row_start=None, d_len=FAKE, d_pages=FAKE, pages_stride=10)
     d.update(kw)
-    return B.PagedBatchDesc(**d)
+    return lib.PagedBatchDesc(**d)
 
 
 def append(B, c, b, **kw):
