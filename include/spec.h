@@ -339,6 +339,48 @@ int spec_sample_accept(void *hip_stream, const float *d_target_logits, const flo
 int spec_set_sampling(spec_ctx *ctx, float temperature, const float *d_uniforms, float *d_target_logits,
                       float *d_draft_logits);
 
+/* Penalties, biases and a grammar's mask on logits, in front of the acceptance rules: what a request asks for beside a
+   temperature.  Row j of sequence b decides the token behind t_1 .. t_j, so these count as emitted in it.  With c the
+   times a token was emitted (positions d_prompt_len[b] .. d_len[b] - 1 of d_tokens, and t_1 .. t_j), and "seen" a token
+   with c > 0 or in the prompt (positions below d_prompt_len[b]), in this order and in fp32:
+     seen tokens:  z = z > 0 ? z / d_repetition[b] : z * d_repetition[b]
+     z = z - (d_frequency[b] * c + (c > 0 ? d_presence[b] : 0))
+     z = z + bias of the token
+     z = -infinity where the mask's bit is 0, whatever was there
+   NULL leaves a rule out.  Token ids and bias ids outside [0, vocab) count for nothing; an id that a sequence's biases
+   list twice has the later one.  A mask holds bit t % 32 of word t / 32 for token t, ceil(vocab / 32) words a row, mask_rows
+   rows a sequence: one for all its rows, or one a row.  A row without any allowed token is -infinity throughout. */
+typedef struct {
+  const int32_t *d_tokens;      /* [B][tokens_stride], the first d_len[b] of each; NULL: nothing seen but proposals */
+  int64_t tokens_stride;
+  const int32_t *d_prompt_len;  /* [B]; NULL: no prompt, all tokens were emitted                    */
+  const int32_t *d_len;         /* [B]                                                              */
+  const float *d_repetition, *d_frequency, *d_presence; /* [B] each                                  */
+  const int32_t *d_bias_ids;    /* [B][n_bias]                                                      */
+  const float *d_bias;          /* [B][n_bias]                                                      */
+  int32_t n_bias;               /* up to 4096                                                       */
+  const uint32_t *d_mask;       /* [B][mask_rows][ceil(vocab / 32)]                                 */
+  int32_t mask_rows;
+} spec_logit_rules;
+
+/* spec_process_logits: the rules on logits the caller has.  d_logits [B][s+1] rows of vocab values of the type `dtype`
+   (SPEC_DTYPE_*), row_stride elements apart (a head whose rows are padded); d_proposals [B][s] (NULL when s = 0, or when
+   proposals do not count); d_out [B][s+1][vocab] fp32, what the acceptance rules take.  d_out may be d_logits itself
+   where the type is fp32 and row_stride = vocab.  Enqueues one kernel on hip_stream (NULL = the default stream), needs no
+   context and no workspace, does not wait.  s <= 15, B <= 65535, vocab <= 2^28 (SPEC_ERR_CAPACITY).
+
+   spec_set_logit_rules: the same rules inside a context, for every following round: they apply to the target's logits
+   before the greedy tokens are taken, or before spec_set_sampling's rule.  The tokens are the context's own (d_tokens,
+   d_prompt_len and d_len NULL, tokens_stride 0); what the rules point to is read by every round, indexed by batch slot, and is
+   the caller's to update between rounds (a grammar's mask between the draft steps and the verify step); mask_rows is 1 or s_max + 1.  Draft
+   steps propose as before: a proposal that the rules forbid is not accepted, what is emitted follows the rules alone.
+   d_target_logits [B_max * (s_max + 1)][vocab] fp32: the caller's buffer for the logits of a round, which the library needs in
+   memory for this (with sampling on, that call's buffer is used and this one may be NULL).  rules NULL: no rules.
+   spec_verify_step's d_logits_or_null then receives the processed logits.  Only between rounds (SPEC_ERR_STATE).          */
+int spec_process_logits(void *hip_stream, const void *d_logits, int32_t dtype, int64_t row_stride, int32_t B, int32_t s,
+                        int32_t vocab, const spec_logit_rules *rules, const int32_t *d_proposals, float *d_out);
+int spec_set_logit_rules(spec_ctx *ctx, const spec_logit_rules *rules, float *d_target_logits);
+
 /* Operators for a caller that runs the target model itself over a paged cache: what its verification pass needs between
    the products, beside the acceptance rules above.  None needs a context; all enqueue on hip_stream (NULL = the default
    stream) and return without waiting; lengths, pages and rows are read on the device, so a call can be captured into a

@@ -33,7 +33,7 @@ EXPORTS = ["spec_last_error", "spec_workspace_bytes", "spec_init", "spec_destroy
            "spec_set_draft_logits", "spec_read_proposals", "spec_greedy_accept_workspace_bytes", "spec_greedy_accept",
            "spec_greedy_accept_noalloc", "spec_set_gemm_tuning", "spec_read_saturation", "spec_sample_tokens",
            "spec_sample_accept", "spec_set_sampling", "spec_paged_append", "spec_paged_attention_workspace_bytes",
-           "spec_paged_attention"]
+           "spec_paged_attention", "spec_process_logits", "spec_set_logit_rules"]
 KCLASS_NAMES = ["gemm_qkv", "gemm_o", "gemm_ffn_in", "gemm_ffn_out", "gemm_head", "attention", "norm", "other",
                 "draft_pass"]
 
@@ -62,6 +62,12 @@ class PagedCacheDesc(C.Structure):
 class PagedBatchDesc(C.Structure):
     _fields_ = [("B", C.c_int32), ("rows", C.c_int32), ("max_rows", C.c_int32), ("max_len", C.c_int32), ("d_row_start", C.c_void_p),
                 ("d_len", C.c_void_p), ("d_pages", C.c_void_p), ("pages_stride", C.c_int32)]
+
+
+class LogitRulesDesc(C.Structure):
+    _fields_ = [("d_tokens", C.c_void_p), ("tokens_stride", C.c_int64), ("d_prompt_len", C.c_void_p), ("d_len", C.c_void_p),
+                ("d_repetition", C.c_void_p), ("d_frequency", C.c_void_p), ("d_presence", C.c_void_p), ("d_bias_ids", C.c_void_p),
+                ("d_bias", C.c_void_p), ("n_bias", C.c_int32), ("d_mask", C.c_void_p), ("mask_rows", C.c_int32)]
 
 
 _vp, _i32, _i32p, _f32p, _i64p = C.c_void_p, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_float), C.POINTER(C.c_int64)
@@ -107,6 +113,8 @@ lib.spec_paged_append.argtypes = [_vp, C.POINTER(PagedCacheDesc), C.POINTER(Page
 lib.spec_paged_attention_workspace_bytes.argtypes = [C.POINTER(PagedCacheDesc), C.POINTER(PagedBatchDesc), _i32, C.POINTER(C.c_size_t)]
 lib.spec_paged_attention.argtypes = [_vp, C.POINTER(PagedCacheDesc), C.POINTER(PagedBatchDesc), _i32, _vp, _i64, C.c_float, _i32, _vp, C.c_size_t,
                                      _vp, _i64]
+lib.spec_process_logits.argtypes = [_vp, _vp, _i32, _i64, _i32, _i32, _i32, C.POINTER(LogitRulesDesc), _vp, _vp]
+lib.spec_set_logit_rules.argtypes = [_vp, C.POINTER(LogitRulesDesc), _vp]
 lib.spec_set_attention_shape.argtypes = [_vp, _i32]
 lib.spec_set_gemm_tuning.argtypes = [_vp, _i32, _i32, _i32]
 lib.spec_kernel_timing.argtypes = [_vp, _i32]
@@ -235,6 +243,51 @@ def spec_sample_accept(target_logits, draft_logits, proposals, uniforms, tempera
           proposals.data_ptr() if s else None, uniforms.data_ptr(), nB, s, V, float(temperature), chosen.data_ptr(), accepted.data_ptr(),
           emitted.data_ptr())
     return chosen, accepted, emitted
+
+
+class LogitRules:
+    """Penalties, biases and masks, device tensors (None: not that rule): tokens [B][n] int32 with prompt_len and length [B] int32,
+    repetition, frequency, presence [B] fp32, bias_ids [B][m] int32 with bias [B][m] fp32, mask [B][rows][ceil(vocab / 32)] int32.
+    Read when a call runs: a program may update them in place between calls."""
+
+    def __init__(self, tokens=None, prompt_len=None, length=None, repetition=None, frequency=None, presence=None, bias_ids=None, bias=None, mask=None):
+        every = (tokens, prompt_len, length, repetition, frequency, presence, bias_ids, bias, mask)
+        self.tensors = every  # must outlive their use
+        self.B = None
+        for t in every:
+            if t is not None:
+                assert t.is_contiguous() or t is tokens and t.dim() == 2 and t.stride(1) == 1
+                self.B = t.shape[0] if self.B is None else self.B
+                assert t.shape[0] == self.B
+        for t, dim, kind in ((tokens, 2, torch.int32), (prompt_len, 1, torch.int32), (length, 1, torch.int32), (repetition, 1, torch.float32),
+                             (frequency, 1, torch.float32), (presence, 1, torch.float32), (bias_ids, 2, torch.int32), (bias, 2, torch.float32),
+                             (mask, 3, torch.int32)):
+            assert t is None or t.dim() == dim and t.dtype == kind
+        assert (bias_ids is None) == (bias is None) and (bias is None or bias.shape == bias_ids.shape)
+        p = lambda t: None if t is None else t.data_ptr()
+        stride = 0 if tokens is None else tokens.stride(0) if self.B > 1 else tokens.shape[1]
+        self.mask_words = None if mask is None else mask.shape[2]
+        self.desc = LogitRulesDesc(p(tokens), stride, p(prompt_len), p(length), p(repetition), p(frequency), p(presence), p(bias_ids), p(bias),
+                                   0 if bias is None else bias.shape[1], p(mask), 0 if mask is None else mask.shape[1])
+
+
+def spec_process_logits(logits, rules, proposals=None, out=None):
+    """logits [B][s+1][V] (fp32, bf16 or fp16, rows may be padded), proposals [B][s] int32 or None -> out [B][s+1][V] fp32, which
+    may be logits itself."""
+    assert logits.dim() == 3 and logits.dtype in _DTYPE_OF
+    nB, q, V = logits.shape
+    row = logits.stride(1) if q > 1 else logits.stride(0) if nB > 1 else V
+    assert logits.stride(2) == 1 and (nB < 2 or logits.stride(0) == q * row)
+    assert rules.B is None or rules.B == nB
+    assert rules.mask_words is None or rules.mask_words == (V + 31) // 32
+    if proposals is not None:
+        assert proposals.dtype == torch.int32 and proposals.shape == (nB, q - 1) and proposals.is_contiguous()
+    if out is None:
+        out = torch.empty((nB, q, V), dtype=torch.float32, device=logits.device)
+    assert out.dtype == torch.float32 and out.shape == (nB, q, V) and out.is_contiguous()
+    _call(logits.device, lib.spec_process_logits, logits.data_ptr(), _DTYPE_OF[logits.dtype], row, nB, q - 1, V, C.byref(rules.desc),
+          proposals.data_ptr() if proposals is not None and q > 1 else None, out.data_ptr())
+    return out
 
 
 _DTYPE_OF = {v: k for k, v in TORCH_DTYPE.items()}
@@ -542,6 +595,20 @@ class Context:
                self.h)
         self._smp = (uniforms, tl, dl)
         return tl, dl
+
+    def spec_set_logit_rules(self, rules):
+        """rules: a LogitRules without tokens, its tensors indexed by batch slot (B_max of them), or None.  Allocates the logits buffer
+        the library needs and returns it ([B_max*(s_max+1)][V]; None without rules)."""
+        if rules is None:
+            _check(lib.spec_set_logit_rules(self.h, None, None), self.h)
+            self._rules = None
+            return None
+        V = self.tgt_desc["vocab"]
+        assert rules.B in (None, self.B_max) and rules.mask_words in (None, (V + 31) // 32)
+        tl = torch.zeros((self.B_max * (self.s_max + 1), V), dtype=torch.float32, device=self.device)
+        _check(lib.spec_set_logit_rules(self.h, C.byref(rules.desc), _dp(tl)), self.h)
+        self._rules = (rules, tl)
+        return tl
 
     def spec_read_saturation(self):
         n = C.c_int64(-1)

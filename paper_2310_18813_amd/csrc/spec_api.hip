@@ -360,6 +360,26 @@ extern "C" int spec_set_sampling(spec_ctx *c, float temperature, const float *d_
   return SPEC_OK;
 }
 
+extern "C" int spec_set_logit_rules(spec_ctx *c, const spec_logit_rules *rules, float *d_target_logits) {
+  if (!c) return fail(nullptr, SPEC_ERR_INVALID_ARG, "spec_set_logit_rules: ctx is null");
+  if (c->draft_j != 0 || c->verified_s >= 0) return fail(c, SPEC_ERR_STATE, "spec_set_logit_rules: a round is in progress");
+  if (!rules) {
+    c->rules_on = false; c->rules = {}; c->rules_tl = nullptr;
+    return SPEC_OK;
+  }
+  if (rules->d_tokens || rules->d_prompt_len || rules->d_len || rules->tokens_stride)
+    return fail(c, SPEC_ERR_INVALID_ARG, "spec_set_logit_rules: the tokens are the context's own");
+  int rc = logit_rules_check("spec_set_logit_rules", rules, c->run.s_max);
+  if (rc) { c->err = g_err; return rc; }
+  if (!d_target_logits && !c->smp_u) return fail(c, SPEC_ERR_INVALID_ARG, "spec_set_logit_rules: a buffer for the target's logits is needed");
+  c->rules = *rules;
+  c->rules.d_tokens = c->st.seq; c->rules.tokens_stride = c->run.L_max;
+  c->rules.d_prompt_len = c->st.P_b; c->rules.d_len = c->st.n;
+  c->rules_tl = d_target_logits;
+  c->rules_on = true;
+  return SPEC_OK;
+}
+
 extern "C" int spec_set_draft_logits(spec_ctx *c, float *d_logits) {
   if (!c) return fail(nullptr, SPEC_ERR_INVALID_ARG, "spec_set_draft_logits: ctx is null");
   if (!c->drf.present) return fail(c, SPEC_ERR_STATE, "spec_set_draft_logits: no draft model");
@@ -750,6 +770,9 @@ static int draft_step(spec_ctx *c, int32_t j, HeadPartials *carry) {
 extern "C" int spec_draft_step(spec_ctx *c, int32_t j) { return draft_step(c, j, nullptr); }
 
 // ------------------------------------------------------------------ verify
+// Rules on logits need the logits in memory: a buffer of their own, or sampling's.
+static bool rules_have_room(const spec_ctx *c) { return !c->rules_on || c->smp_u || c->rules_tl; }
+static const char RULES_NO_ROOM[] = "the rules on logits have no buffer: they were set without one, and sampling is off now";
 static int verify_step(spec_ctx *c, int32_t s, float *d_logits_or_null, const HeadPartials &last) {
   if (!c) return fail(nullptr, SPEC_ERR_INVALID_ARG, "spec_verify_step: ctx is null");
   if (!c->active) return fail(c, SPEC_ERR_STATE, "spec_verify_step: no batch; call spec_reset first");
@@ -759,15 +782,22 @@ static int verify_step(spec_ctx *c, int32_t s, float *d_logits_or_null, const He
     return fail(c, SPEC_ERR_STATE, "spec_verify_step: s=%d needs %d draft steps first, %d were run", s, s, c->draft_j);
   if (c->draft_j != 0 && c->draft_j != s)
     return fail(c, SPEC_ERR_STATE, "spec_verify_step: %d draft steps were run for s=%d", c->draft_j, s);
+  if (!d_logits_or_null && !rules_have_room(c)) return fail(c, SPEC_ERR_STATE, "spec_verify_step: %s", RULES_NO_ROOM);
   int fill;
   int rc = ensure_proposals(c, s, "spec_verify_step", fill);
   if (rc) return rc;
   PassArgs pa{PASS_VERIFY, c->B, s + 1, 0};
   pa.fill = fill;
   pa.last = last;
-  float *lg = d_logits_or_null ? d_logits_or_null : c->smp_u ? c->smp_tl : nullptr;
+  float *lg = d_logits_or_null ? d_logits_or_null : c->smp_u ? c->smp_tl : c->rules_on ? c->rules_tl : nullptr;
   rc = forward_pass(c, c->tgt, pa, HEAD_ALL, lg, c->st.a, c->run.s_max + 1, c->n_ub - 1 + s);
   if (rc) return rc;
+  if (c->rules_on) {
+    KScope k(c, SPEC_KCLASS_OTHER);
+    launch_process_logits(lg, SPEC_DTYPE_F32, c->tgt.desc.vocab, c->B, s, c->tgt.desc.vocab, c->rules, c->st.t, c->run.s_max, lg, c->stream);
+    if (!c->smp_u) launch_argmax_rows(lg, c->B * (s + 1), c->tgt.desc.vocab, s + 1, c->run.s_max + 1, c->st.a, c->stream);
+    HIPCHK(c, hipGetLastError());
+  }
   if (c->smp_u) {  // the sampling rule in place of the arg-max: row j decides the token at position n_b + j
     KScope k(c, SPEC_KCLASS_OTHER);
     launch_sample_verify(lg, c->smp_dl, c->run.B_max, c->B, s, c->tgt.desc.vocab, c->smp_T, c->st.t, c->run.s_max, c->seq_s,
@@ -802,6 +832,7 @@ extern "C" int spec_round(spec_ctx *c, int32_t s, int32_t n_rounds) {
   if (s < 0 || s > c->run.s_max) return fail(c, SPEC_ERR_CAPACITY, "spec_round: s=%d outside 0..s_max=%d", s, c->run.s_max);
   if (n_rounds < 0) return fail(c, SPEC_ERR_INVALID_ARG, "spec_round: n_rounds is negative");
   if (c->draft_j != 0 || c->verified_s >= 0) return fail(c, SPEC_ERR_STATE, "spec_round: a round is already in progress");
+  if (!rules_have_room(c)) return fail(c, SPEC_ERR_STATE, "spec_round: %s", RULES_NO_ROOM);
   const bool ext = c->run.proposal_mode == SPEC_PROPOSALS_EXTERNAL;
   if (ext && s > 0 && !c->prop_table && !(n_rounds == 1 && c->proposals_ready))
     return fail(c, SPEC_ERR_STATE, "spec_round: external proposals need a table (spec_set_proposal_table)");

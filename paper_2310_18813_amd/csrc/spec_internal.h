@@ -149,6 +149,10 @@ struct spec_ctx {
   float smp_T = 0.f;
   const float *smp_u = nullptr;
   float *smp_tl = nullptr, *smp_dl = nullptr;
+  // rules on the target's logits (off while rules_on is false) and the caller's buffer for them [M_max][vocab]
+  bool rules_on = false;
+  spec_logit_rules rules{};
+  float *rules_tl = nullptr;
   int attn_shape = 0;
   int gemm_tune = 0;      // GemmTune bits (spec_set_gemm_tuning)
   int n_cu = 256;         // compute units of the context's device
@@ -226,6 +230,10 @@ void launch_sample_rows(const float *logits, int rows, int V, float temperature,
 void launch_sample_verify(const float *tl, const float *dl, int d_rows, int B, int s, int V, float temperature,
                           const int32_t *t, int t_stride, const int32_t *seq_s, const float *u, const int32_t *n, int u_rows,
                           int32_t *a, int a_stride, hipStream_t st, int32_t *accepted = nullptr, int32_t *emitted = nullptr);
+// penalties, biases and masks (kernels_logits.hip): the caller has checked every argument
+int logit_rules_check(const char *who, const spec_logit_rules *r, int s);
+void launch_process_logits(const void *logits, int dtype, int64_t row_stride, int B, int s, int V, const spec_logit_rules &r,
+                           const int32_t *t, int t_stride, float *out, hipStream_t st);
 void launch_prefill_groups(const spec_ctx *c, int b0, int B, int q, hipStream_t st);
 void launch_copy_proposals(spec_ctx *c, const int32_t *d_tok, int s, hipStream_t st);
 void launch_state_reset(spec_ctx *c, const int32_t *d_prompt, int P_stride, bool ragged, hipStream_t st);

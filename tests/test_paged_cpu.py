@@ -81,3 +81,20 @@ def test_attention_arguments(B):
     assert attend(B, cache(B), long, ws=FAKE, wb=n.value - 1) == B.ERR_WORKSPACE
     many = batch(B, rows=1 << 29, max_rows=1 << 29, d_row_start=FAKE)
     assert attend(B, cache(B), many) == B.ERR_CAPACITY
+
+
+def test_logit_rules_arguments(B):
+    def call(rules=None, logits=FAKE, dtype=B.DTYPE_F32, stride=1000, nB=2, s=3, V=1000, t=FAKE, out=FAKE + 64, **kw):
+        r = rules if rules is not None else B.LogitRulesDesc(**kw)
+        return B.lib.spec_process_logits(None, logits, dtype, stride, nB, s, V, C.byref(r) if r else None, t, out)
+    for kw in (dict(nB=-1), dict(s=-1), dict(V=0), dict(dtype=7), dict(stride=999), dict(rules=False), dict(n_bias=-1), dict(n_bias=3),
+               dict(n_bias=3, d_bias=FAKE), dict(d_mask=FAKE, mask_rows=2), dict(d_mask=FAKE), dict(d_tokens=FAKE, tokens_stride=9),
+               dict(d_tokens=FAKE, d_len=FAKE), dict(logits=None), dict(out=None), dict(logits=FAKE + 2), dict(out=FAKE + 2),
+               dict(dtype=B.DTYPE_BF16, out=FAKE), dict(stride=1004, out=FAKE)):
+        assert call(**kw) == B.ERR_INVALID_ARG, kw
+        assert b"spec_process_logits" in B.lib.spec_last_error(None)
+    for kw in (dict(s=16), dict(nB=65536), dict(V=(1 << 28) + 1, stride=1 << 29), dict(n_bias=4097, d_bias=FAKE, d_bias_ids=FAKE),
+               dict(d_tokens=FAKE, d_len=FAKE, tokens_stride=1 << 30)):
+        assert call(**kw) == B.ERR_CAPACITY, kw
+    assert call(nB=0, logits=None, out=None) == B.OK
+    assert B.lib.spec_set_logit_rules(None, None, None) == B.ERR_INVALID_ARG
