@@ -17,16 +17,21 @@
 #include "paged.h"
 #include <algorithm>
 #include <cmath>
+#include <mutex>
 #include <type_traits>
 
 namespace spec {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8_v;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8_v;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_v;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_v;
+typedef __attribute__((ext_vector_type(2))) float f32x2_v;
 typedef __attribute__((ext_vector_type(4))) float f32x4_v;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_v;
 
 constexpr int PA_SLOTS = 1024;    // workgroups that a pass is cut into where it is long enough
+constexpr int PC_SLOTS = 2048;    // the same for tiles of many rows
 constexpr int PA_CHUNK_MIN = 512; // positions of the shortest chunk: a shorter context is not worth a second kernel
 constexpr int PA_WAVES = 4;
 
@@ -43,6 +48,10 @@ struct AttendArgs {
 
 // ------------------------------------------------------------------ work
 struct Work { int b, tile, chunk, chunks, base, chunk_len; PagedSeq s; };
+__device__ __forceinline__ Work in_scalars(const Work &w) {
+  auto f = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  return Work{f(w.b), f(w.tile), f(w.chunk), f(w.chunks), f(w.base), f(w.chunk_len), PagedSeq{f(w.s.row0), f(w.s.n), f(w.s.kv)}};
+}
 
 __device__ __forceinline__ int seq_tiles(const AttendArgs &a, const PagedSeq &s, int R) { return (s.n * a.G + R - 1) / R; }
 // positions that a tile of the sequence can need, at most
@@ -97,16 +106,14 @@ __device__ __forceinline__ bool find_work(const AttendArgs &a, int R, int unit, 
     const int t = seq_tiles(a, s, R), c = max(1, (seq_span(a, s, R) + len - 1) / len), n = TILES ? t : t * c;
     if (unit < at + n) {
       const int u = unit - at;
-      w.b = __builtin_amdgcn_readfirstlane(b);
-      w.chunks = __builtin_amdgcn_readfirstlane(c);
+      w.b = b;
+      w.chunks = c;
       // the last rows of a sequence see the most: their tiles start first
-      w.tile = __builtin_amdgcn_readfirstlane(TILES ? t - 1 - u : t - 1 - u % t);
-      w.chunk = __builtin_amdgcn_readfirstlane(TILES ? 0 : u / t);
-      w.base = __builtin_amdgcn_readfirstlane(TILES ? base + u : 0);  // the tile's chunk j is unit base + j * tiles
+      w.tile = TILES ? t - 1 - u : t - 1 - u % t;
+      w.chunk = TILES ? 0 : u / t;
+      w.base = TILES ? base + u : 0;  // the tile's chunk j is unit base + j * tiles
       w.chunk_len = len;
-      w.s.row0 = __builtin_amdgcn_readfirstlane(s.row0);
-      w.s.n = __builtin_amdgcn_readfirstlane(s.n);
-      w.s.kv = __builtin_amdgcn_readfirstlane(s.kv);
+      w.s = s;
       return true;
     }
     at += n;
@@ -128,8 +135,8 @@ template <> struct Mat<bf16_t> {
   static __device__ __forceinline__ f32x4_v run(u32x4_v a, u32x4_v b, f32x4_v c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_v, a), __builtin_bit_cast(bf16x8_v, b), c, 0, 0, 0);
   }
-  static __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-    return (uint32_t)f32_to_bf16_bits(lo) | ((uint32_t)f32_to_bf16_bits(hi) << 16);
+  static __device__ __forceinline__ uint32_t pack2(float lo, float hi) {  // to nearest, one instruction
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_v){lo, hi}, bf16x2_v));
   }
 };
 template <> struct Mat<f16_t> {
@@ -137,11 +144,7 @@ template <> struct Mat<f16_t> {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_v, a), __builtin_bit_cast(f16x8_v, b), c, 0, 0, 0);
   }
   static __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-    const f16_t a = (f16_t)lo, b = (f16_t)hi;
-    uint16_t ua, ub;
-    __builtin_memcpy(&ua, &a, 2);
-    __builtin_memcpy(&ub, &b, 2);
-    return (uint32_t)ua | ((uint32_t)ub << 16);
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_v){lo, hi}, f16x2_v));
   }
 };
 
@@ -200,10 +203,18 @@ __device__ __forceinline__ u32x4_v value_operand(const Step<T, HD> &f, int ht) {
   return x;
 }
 
-// whether a word of cached values holds an infinity or a NaN
-template <class T> __device__ __forceinline__ bool not_finite(uint32_t w) {
+// Takes infinities and NaN out of a word of cached values; whether there were any.
+template <class T> __device__ __forceinline__ bool drop_odd(uint32_t &w) {
   constexpr uint32_t e = sizeof(T) == 4 ? 0x7f800000u : std::is_same<T, bf16_t>::value ? 0x7f80u : 0x7c00u;
-  return (w & e) == e || (sizeof(T) == 2 && (w >> 16 & e) == e);
+  const bool lo = (w & e) == e, hi = sizeof(T) == 2 && (w >> 16 & e) == e;
+  if (sizeof(T) == 4) w = lo ? 0u : w;
+  else w &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+  return lo || hi;
+}
+// The value if it is infinite or NaN, else zero.
+template <class T> __device__ __forceinline__ float only_odd(T t) {
+  const float v = Conv<T>::ld(&t, 0);
+  return fabsf(v) < INFINITY ? 0.f : v;
 }
 
 // ------------------------------------------------------------------ few query rows a tile: the waves share the positions
@@ -218,6 +229,7 @@ __global__ __launch_bounds__(256) void k_paged_attend(AttendArgs a) {
   const int Hk = a.p.n_kv_heads, unit = blockIdx.x / Hk, hk = blockIdx.x % Hk;
   Work w;
   if (!find_work<false>(a, R, unit, w)) return;
+  w = in_scalars(w);
   const PagedSeq s = w.s;
   int lo, hi;
   tile_range(a, s, w.tile, R, lo, hi);
@@ -267,6 +279,7 @@ __global__ __launch_bounds__(256) void k_paged_attend(AttendArgs a) {
     load_step<T, HD>(cur, a.p, head_at, pk, pv, ks0, r, g);
   }
   int j = 0;
+  bool odd = false;
   for (int ks = ks0; ks < k_end; ks += 128) {
     if (ks + 128 < k_end) {
       if (++j == 16) {
@@ -288,24 +301,13 @@ __global__ __launch_bounds__(256) void k_paged_attend(AttendArgs a) {
         for (int x = 0; x < St::VW; ++x) cur.v[i][x] = live ? cur.v[i][x] : 0u;
       }
     }
-    // Positions that some rows of the tile see and others do not: a weight of zero does not keep an infinity or a NaN out of the
-    // product, so such positions leave it and are added below for the rows that see them.
-    uint32_t odd = 0;  // bit 8g + i
+    // Positions that some of the tile's rows see and others do not: a weight of zero does not keep an infinity or a NaN out of a
+    // product, so such values leave here and are added at the end for the rows that see them.
     if (!whole && i0 != i1) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        bool any = false;
+      for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int x = 0; x < St::VW; ++x) any |= not_finite<T>(cur.v[i][x]);
-        const unsigned long long lanes = __ballot(any);
-        if (lanes) {
-#pragma unroll
-          for (int x = 0; x < 4; ++x) odd |= (lanes >> (16 * x) & 0xffff) ? 1u << (8 * x + i) : 0u;
-          const bool drop = odd >> (8 * g + i) & 1;
-#pragma unroll
-          for (int x = 0; x < St::VW; ++x) cur.v[i][x] = drop ? 0u : cur.v[i][x];
-        }
-      }
+        for (int x = 0; x < St::VW; ++x) odd |= drop_odd<T>(cur.v[i][x]);
     }
     float p[QT][8];
 #pragma unroll
@@ -357,28 +359,28 @@ __global__ __launch_bounds__(256) void k_paged_attend(AttendArgs a) {
             acc[t][ht] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(cur.v[i][ht]), p[t][i], acc[t][ht], 0, 0, 0);
       }
     }
-    if (odd) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        for (int x = 0; x < 4; ++x) {
-          if (!(odd >> (8 * x + i) & 1)) continue;
-          const int page = __shfl(pv, 16 * x, 64), key = ks + 8 * x + i;
-          const T *src = (const T *)a.p.v + head_at + page * a.p.page_stride + (key & ((1 << a.p.page_shift) - 1)) * a.p.pos_stride + VE * 4 * g;
-#pragma unroll
-          for (int t = 0; t < QT; ++t) {
-            const float wt = __shfl(p[t][i], 16 * x + r, 64);
-            if (wt == 0.f) continue;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-              for (int ht = 0; ht < HT; ++ht) acc[t][ht][e] += wt * Conv<T>::ld(src, VE * e + ht);
-          }
-        }
-      }
-    }
     if (AHEAD) cur = nxt;
     else if (ks + 128 < k_end) load_step<T, HD>(cur, a.p, head_at, pk_n, pv_n, ks + 128, r, g);
     pv = pv_n;
+  }
+
+  if (__any(odd)) {  // this wave's steps of the positions outside [see_lo, see_hi) again
+    for (int ks = ks0; ks < k_end; ks += 128) {
+      if (ks >= see_lo && ks + 32 <= min(see_hi, k_end)) continue;
+      for (int key = ks; key < min(ks + 32, k_end); ++key) {
+        const int page = paged_page(a.p, w.b, key);
+        if (page < 0) continue;
+        const T *src = (const T *)a.p.v + head_at + page * a.p.page_stride + (key & ((1 << a.p.page_shift) - 1)) * a.p.pos_stride + 4 * VE * g;
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+          if (key > pos[t] || (a.window && key <= pos[t] - a.window)) continue;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int ht = 0; ht < HT; ++ht) acc[t][ht][e] += only_odd<T>(src[VE * e + ht]);
+        }
+      }
+    }
   }
 
   // the waves' maxima and sums, then their outputs, 16 query rows at a time
@@ -429,6 +431,267 @@ __global__ __launch_bounds__(256) void k_paged_attend(AttendArgs a) {
   }
 }
 
+// ------------------------------------------------------------------ many query rows: the waves share the cached rows through LDS
+typedef __attribute__((ext_vector_type(16))) float f32x16_v;
+template <class T> __device__ __forceinline__ f32x16_v mat32(u32x4_v a, u32x4_v b, f32x16_v c) {
+  if constexpr (std::is_same<T, bf16_t>::value)
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_v, a), __builtin_bit_cast(bf16x8_v, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_v, a), __builtin_bit_cast(f16x8_v, b), c, 0, 0, 0);
+}
+// 16 bytes a lane from its own address to LDS byte `lds` + 16 lane
+__device__ __forceinline__ void lanes_to_lds(const void *p, unsigned lds) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(lds), "v"(p) : "memory");
+}
+// The largest of 16.  Written as fmaxf, every score is first brought to canonical form by an instruction of its own.
+__device__ __forceinline__ float max16(const f32x16_v &x) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3\n\tv_max3_f32 %0, %0, %4, %5\n\tv_max3_f32 %0, %0, %6, %7\n\tv_max3_f32 %0, %0, %8, %9\n\t"
+      "v_max3_f32 %0, %0, %10, %11\n\tv_max3_f32 %0, %0, %12, %13\n\tv_max3_f32 %0, %0, %14, %15\n\tv_max_f32 %0, %0, %16"
+      : "=&v"(r)
+      : "v"(x[0]), "v"(x[1]), "v"(x[2]), "v"(x[3]), "v"(x[4]), "v"(x[5]), "v"(x[6]), "v"(x[7]), "v"(x[8]), "v"(x[9]), "v"(x[10]), "v"(x[11]),
+        "v"(x[12]), "v"(x[13]), "v"(x[14]), "v"(x[15]));
+  return r;
+}
+__device__ __forceinline__ float max_of_halves(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
+
+// A workgroup of four waves takes 128 query rows, 32 a wave, and walks the positions in tiles of KT = 64 (heads of 128) or 128 (of 64): 16 KB
+// of keys and 16 KB of values, in LDS in operand order, twice.  32x32x16 products: a lane owns one query (lane % 32) and half of
+// every 16 keys, so a row's maximum takes one exchange.  Keys go straight to LDS, [key][unit of 16 bytes], a row's units exchanged by its number so
+// that reading one unit of 32 rows meets every bank; of values a thread loads 8 positions of 4 elements and turns them round on
+// the way to LDS.  The maximum follows the scores only when they have grown
+// by 2^8: weights up to 2^8 are as exact in 16 bits as weights up to 1, the sums are fp32, and most tiles then rescale nothing.
+constexpr int PC_ROWS = 128;
+constexpr int PC_LDS = 4 * 16384;
+
+template <class T, int HD>
+__global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendArgs a) {
+  constexpr int NC = HD / 8, KK = HD / 16, DT = HD / 32, KT = 8 * 128 / NC, VC = HD / 4, IPT = 32 / VC;
+  extern __shared__ __attribute__((aligned(16))) u32x4_v pc_smem[];  // [2] keys [KT][NC], [2] values [KT / 16][DT][2][32]
+  const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
+  const int Hk = a.p.n_kv_heads, unit = blockIdx.x / Hk, hk = blockIdx.x % Hk;
+  Work w;
+  if (!find_work<false>(a, PC_ROWS, unit, w)) return;
+  w = in_scalars(w);
+  const PagedSeq s = w.s;
+  int lo, hi;
+  tile_range(a, s, w.tile, PC_ROWS, lo, hi);
+  const int k_begin = lo + w.chunk * w.chunk_len, k_end = hi - k_begin > w.chunk_len ? k_begin + w.chunk_len : hi;
+  const int rows = s.n * a.G, p0 = s.kv - s.n;
+
+  // this lane's query, and what the wave's queries see: all of them [see_lo, see_hi), any of them [any_lo, any_hi)
+  const int f0 = w.tile * PC_ROWS + 32 * wv, f = f0 + col, qi = f / a.G;
+  const bool on = f < rows;
+  const int pos = on ? p0 + qi : -1;
+  const int first = p0 + f0 / a.G, last = p0 + min(f0 + 31, rows - 1) / a.G;
+  const int see_hi = first + 1, see_lo = a.window ? last - a.window + 1 : 0, any_hi = f0 < rows ? last + 1 : 0, any_lo = a.window ? first - a.window + 1 : 0;
+  u32x4_v q[KK];
+  {
+    const T *src = (const T *)a.q + (on ? (s.row0 + qi) * a.q_stride + (hk * a.G + f - qi * a.G) * HD : 0) + 8 * h;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) q[kk] = on ? *(const u32x4_v *)(src + 16 * kk) : (u32x4_v){0, 0, 0, 0};
+  }
+
+  // staging
+  const int vc = threadIdx.x % VC, kg = threadIdx.x / VC, mask = (1 << a.p.page_shift) - 1;
+  const int64_t head_at = hk * a.p.head_stride;
+  const T *k_base = (const T *)a.p.k + head_at, *v_base = (const T *)a.p.v + head_at + 4 * vc;
+  auto page_at = [&](int pos) { return pos < k_end ? paged_page(a.p, w.b, pos) : -1; };
+  // Row 32 u + 16 x + 8 y + 4 z + e of a key tile holds key 32 u + 16 x + 8 z + 4 y + e.  Wave instruction `it` fills 64 / NC rows; its
+  // lanes' keys lie in one of two groups of eight positions, kgrp[it's].
+  const int kgrp0 = NC == 16 ? 2 * wv : 4 * wv + (lane >> 5), kgrp1 = kgrp0 + (NC == 16 ? 1 : 2);
+  const int krow = NC == 16 ? 16 * wv + (lane >> 4) : 32 * wv + 8 * (lane >> 5) + (lane >> 3 & 3);  // key of it = 0
+  uint32_t x[8][2];
+  int x_page;
+  struct Pages { int k[2], v; };
+  auto pages_of = [&](int ks) { return Pages{{page_at(ks + 8 * kgrp0), page_at(ks + 8 * kgrp1)}, page_at(ks + 8 * kg)}; };
+  auto fetch = [&](int ks, const Pages &pg, int kbuf) {
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+      const int key = krow + (NC == 16 ? 8 * (it & 1) + 4 * (it >> 1) : 16 * (it >> 1) + 4 * (it & 1));
+      const int unit = NC == 16 ? (lane ^ (lane >> 4)) % 16 ^ 4 * it : (lane ^ (lane >> 3)) % 8;  // by the row's number
+      const T *src = k_base + max(pg.k[NC == 16 ? it & 1 : it >> 1], 0) * a.p.page_stride + ((ks + key) & mask) * a.p.pos_stride + 8 * unit;
+      lanes_to_lds(src, (unsigned)((kbuf * 1024 + (wv * 4 + it) * 64) * 16));
+    }
+    const T *src = v_base + max(pg.v, 0) * a.p.page_stride + ((ks + 8 * kg) & mask) * a.p.pos_stride;
+    x_page = pg.v;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) __builtin_memcpy(x[i], __builtin_assume_aligned(src + i * a.p.pos_stride, 8), 8);
+  };
+  // Positions that some of the tile's rows see and others do not (those outside [all_lo, all_hi)): a weight of zero does not keep an infinity
+  // or a NaN out of a product, so such values leave here and are added at the end for the rows that see them.
+  const int all_hi = p0 + w.tile * PC_ROWS / a.G + 1, all_lo = a.window ? p0 + min(w.tile * PC_ROWS + PC_ROWS - 1, rows - 1) / a.G - a.window + 1 : 0;
+  bool odd = false;
+  auto store = [&](int ks, int vbuf) {
+    const int live = x_page < 0 ? 0 : k_end - (ks + 8 * kg);  // positions behind the end hold anything
+    if (live < 8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { x[i][0] = i < live ? x[i][0] : 0u; x[i][1] = i < live ? x[i][1] : 0u; }
+    }
+    if (ks + KT > all_hi || ks < all_lo) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { odd |= drop_odd<T>(x[i][0]); odd |= drop_odd<T>(x[i][1]); }
+    }
+    u32x4_v *vb = pc_smem + (2 + vbuf) * 1024 + (kg >> 1) * DT * 64 + (kg & 1) * 32 + vc;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      u32x4_v y;
+#pragma unroll
+      for (int d = 0; d < 4; ++d) y[d] = __builtin_amdgcn_perm(x[2 * d + 1][i / 2], x[2 * d][i / 2], (i & 1) ? 0x07060302u : 0x05040100u);
+      vb[(i / IPT) * 64 + VC * (i % IPT)] = y;
+    }
+  };
+  // loads to LDS have landed, reads of LDS are done; behind the barrier everyone's
+  auto meet = [&]() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+
+  float m = -INFINITY, l = 0.f;
+  const float grow = 8.f / a.sl2;
+  f32x16_v acc[DT];
+#pragma unroll
+  for (int j = 0; j < DT; ++j)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[j][e] = 0.f;
+
+  // score e of sc[u]: key ks + 32 u + 16 (e / 8) + 8 h + e % 8
+  f32x16_v sc[2];
+  auto key_products = [&](const u32x4_v *kb) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sc[u][e] = 0.f;
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) sc[u] = mat32<T>(kb[(32 * u + col) * NC + ((2 * kk + h) ^ (col & (NC - 1)))], q[kk], sc[u]);
+    }
+  };
+  // the maximum follows where it has to; -> what is taken off the scaled scores
+  auto follow = [&]() {
+    const float top = max_of_halves(fmaxf(max16(sc[0]), max16(sc[1])));
+    if (__any(top > m + grow)) {
+      const float mn = fmaxf(m, top), corr = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * a.sl2);
+      m = mn;
+      l *= corr;
+#pragma unroll
+      for (int j = 0; j < DT; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[j][e] *= corr;
+    }
+    return m == -INFINITY ? 0.f : m * a.sl2;
+  };
+  auto weights = [&](int y, float off) {  // of the 16 keys y of a step
+    u32x4_v p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float p0 = __builtin_amdgcn_exp2f(fmaf(sc[y / 2][8 * (y & 1) + 2 * i], a.sl2, -off));
+      const float p1 = __builtin_amdgcn_exp2f(fmaf(sc[y / 2][8 * (y & 1) + 2 * i + 1], a.sl2, -off));
+      l += p0 + p1;
+      p[i] = Mat<T>::pack2(p0, p1);
+    }
+    return p;
+  };
+  // Tile t lies in buffers t % 2.  Lane i of a wave also looks whether the i-th eight positions of a tile are there at all.
+  auto there_at = [&](int ks) { return lane < KT / 8 ? page_at(ks + 8 * lane) : -1; };
+  unsigned present = 0;
+  Pages pages{{-1, -1}, -1};
+  if (k_begin < k_end) {
+    const int there = there_at(k_begin);
+    fetch(k_begin, pages_of(k_begin), 0);
+    pages = pages_of(k_begin + KT);
+    store(k_begin, 0);
+    present = (unsigned)__ballot(there >= 0);
+  }
+  meet();
+  int buf = 0;
+  for (int ks0 = k_begin; ks0 < k_end; ks0 += KT, buf ^= 1) {
+    // The next tile's loads land while this one is worked on.  Behind the last tile they bring page 0's rows, which nothing reads: no branch
+    // keeps the address arithmetic from the products' shadow.
+    fetch(ks0 + KT, pages, buf ^ 1);
+    pages = pages_of(ks0 + 2 * KT);
+    const int there = there_at(ks0 + KT);
+    const u32x4_v *kb = pc_smem + buf * 1024, *vb = pc_smem + (2 + buf) * 1024 + h * 32 + col;
+#pragma unroll
+    for (int step = 0; step < KT / 64; ++step) {
+      const int ks = ks0 + 64 * step;
+      const unsigned here = present >> (8 * step) & 0xff;
+      const u32x4_v *ksrc = kb + 64 * step * NC, *vs = vb + step * 4 * DT * 64;
+      if (ks >= any_hi || ks + 64 <= any_lo || ks >= k_end) continue;
+      key_products(ksrc);
+      if (ks < see_lo || ks + 64 > min(see_hi, k_end) || here != 0xff) {
+        const int from = a.window ? pos - a.window + 1 : 0;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int group = 4 * u + 2 * (e >> 3) + h, key = ks + 8 * group + (e & 7);
+            sc[u][e] = key <= pos && key >= from && key < k_end && (here >> group & 1) ? sc[u][e] : -INFINITY;
+          }
+      }
+      const float off = follow();
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        const u32x4_v p = weights(y, off);
+#pragma unroll
+        for (int j = 0; j < DT; ++j) acc[j] = mat32<T>(vs[(y * DT + j) * 64], p, acc[j]);
+      }
+    }
+    store(ks0 + KT, buf ^ 1);
+    present = (unsigned)__ballot(there >= 0);
+    meet();
+  }
+
+  l += __shfl_xor(l, 32, 64);
+  uint32_t *flags = (uint32_t *)pc_smem;  // nothing reads the tiles any more
+  if (lane == 0) flags[wv] = 0;
+  if (odd) flags[wv] = 1;
+  meet();
+  if (flags[0] | flags[1] | flags[2] | flags[3]) {
+    const int from = a.window ? pos - a.window + 1 : 0;
+    for (int key = k_begin; key < k_end; ++key) {
+      if (key >= all_lo && key < all_hi) { key = all_hi - 1; continue; }
+      const int page = page_at(key);
+      if (page < 0 || key > pos || key < from) continue;
+      const T *src = (const T *)a.p.v + head_at + page * a.p.page_stride + (key & mask) * a.p.pos_stride;
+#pragma unroll
+      for (int j = 0; j < DT; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int row = 8 * (e >> 2) + 4 * h + (e & 3);
+          acc[j][e] += only_odd<T>(src[4 * (row % VC) + j * IPT + row / VC]);
+        }
+    }
+  }
+  if (!on) return;
+  // element 4 c + i of the query lies in tile i / IPT, row c + VC (i % IPT); a lane holds the rows 8 (e / 4) + 4 h + e % 4
+  const bool several = w.chunks > 1;
+  const int64_t at = (int64_t)blockIdx.x * PC_ROWS + 32 * wv + col;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T *dst = (T *)a.out + (s.row0 + qi) * a.out_stride + (hk * a.G + f - qi * a.G) * HD;
+  if (several && h == 0) { a.ml[at * 2] = m; a.ml[at * 2 + 1] = l; }
+#pragma unroll
+  for (int x = 0; x < VC / 8; ++x) {  // rows 8 x + 4 h + y: 16 elements in a row
+    const int d = 4 * (8 * x + 4 * h);
+    float o[16];
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[4 * y + i] = acc[i / IPT][4 * (x + VC / 8 * (i % IPT)) + y];
+    if (several) {
+#pragma unroll
+      for (int y = 0; y < 4; ++y) *(f32x4_v *)(a.part + at * HD + d + 4 * y) = (f32x4_v){o[4 * y], o[4 * y + 1], o[4 * y + 2], o[4 * y + 3]};
+    } else {
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        u32x4_v v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = Mat<T>::pack2(l == 0.f ? 0.f : o[8 * y + 2 * i] * inv, l == 0.f ? 0.f : o[8 * y + 2 * i + 1] * inv);
+        *(u32x4_v *)(dst + d + 8 * y) = v;
+      }
+    }
+  }
+}
+
 // Joins the chunks of a tile: a workgroup takes 16 query rows of a tile, a thread VE elements of one.
 template <class T, int HD, int QT>
 __global__ __launch_bounds__(256) void k_paged_join(AttendArgs a) {
@@ -462,17 +725,18 @@ __global__ __launch_bounds__(256) void k_paged_join(AttendArgs a) {
 }
 
 // ------------------------------------------------------------------ launch
-struct Shape { int qt, R; int64_t tiles, units; bool join; };
+struct Shape { int qt, R, slots; int64_t tiles, units; bool join; };
 
 // Query rows of a tile: as few as hold a sequence's, since a tile reads the cache once for all of its rows.
 static Shape attend_shape(const spec_paged_cache *c, const spec_paged_batch *b, int n_q) {
   Shape s;
   const int64_t G = n_q / c->n_kv_heads, per = (int64_t)b->max_rows * G;
-  s.qt = per <= 16 ? 1 : per <= 32 || c->dtype == SPEC_DTYPE_F32 ? 2 : 4;
+  s.qt = per <= 16 ? 1 : per <= 32 || c->dtype == SPEC_DTYPE_F32 ? 2 : per <= 64 ? 4 : PC_ROWS / 16;
   s.R = 16 * s.qt;
   s.tiles = std::min((int64_t)b->B * ((per + s.R - 1) / s.R), (int64_t)b->rows * G / s.R + b->B);
   s.join = b->max_len > PA_CHUNK_MIN;
-  s.units = s.tiles + (s.join ? PA_SLOTS / c->n_kv_heads + 1 : 0);
+  s.slots = std::max(1, (s.R == PC_ROWS ? PC_SLOTS : PA_SLOTS) / c->n_kv_heads);
+  s.units = s.tiles + (s.join ? s.slots : 0);
   return s;
 }
 static size_t attend_bytes(const spec_paged_cache *c, const Shape &s) {
@@ -485,16 +749,37 @@ static int attend_check(const char *who, const spec_paged_cache *c, const spec_p
     return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: n_q_heads=%d is not a multiple of n_kv_heads=%d", who, n_q, c->n_kv_heads);
   a.G = n_q / c->n_kv_heads;
   if ((int64_t)b->rows * a.G >= 1 << 30) return fail_noctx(SPEC_ERR_CAPACITY, "%s: more than 2^30 query rows of a key head", who);
-  if (b->B == 0 || b->rows == 0) { s = Shape{1, 16, 0, 0, false}; return SPEC_OK; }
+  if (b->B == 0 || b->rows == 0) { s = Shape{1, 16, 1, 0, 0, false}; return SPEC_OK; }
   s = attend_shape(c, b, n_q);
   if (s.units * c->n_kv_heads * 256 >= (int64_t)1 << 32 || s.tiles * c->n_kv_heads * s.qt * 256 >= (int64_t)1 << 32)
     return fail_noctx(SPEC_ERR_CAPACITY, "%s: %lld tiles of %d key heads are beyond one launch", who, (long long)s.units, c->n_kv_heads);
   return SPEC_OK;
 }
 
+// More LDS than 64 KB has to be asked for, once on every device.
+static hipError_t allow_chunk_lds() {
+  static std::mutex mutex;
+  static bool done[64];
+  int dev = -1;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  std::lock_guard<std::mutex> lock(mutex);
+  if (dev >= 0 && dev < 64 && done[dev]) return hipSuccess;
+  const void *kernels[4] = {(const void *)k_paged_chunk<bf16_t, 64>, (const void *)k_paged_chunk<bf16_t, 128>,
+                            (const void *)k_paged_chunk<f16_t, 64>, (const void *)k_paged_chunk<f16_t, 128>};
+  for (const void *k : kernels) {
+    e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, PC_LDS);
+    if (e != hipSuccess) return e;
+  }
+  if (dev >= 0 && dev < 64) done[dev] = true;
+  return hipSuccess;
+}
+
 template <class T, int HD, int QT>
 static void attend_launch(const AttendArgs &a, const Shape &s, hipStream_t st) {
-  hipLaunchKernelGGL((k_paged_attend<T, HD, QT>), dim3((unsigned)(s.units * a.p.n_kv_heads)), dim3(256), 0, st, a);
+  const dim3 grid((unsigned)(s.units * a.p.n_kv_heads));
+  if constexpr (QT == PC_ROWS / 16) hipLaunchKernelGGL((k_paged_chunk<T, HD>), grid, dim3(256), PC_LDS, st, a);
+  else hipLaunchKernelGGL((k_paged_attend<T, HD, QT>), grid, dim3(256), 0, st, a);
   if (s.join) hipLaunchKernelGGL((k_paged_join<T, HD, QT>), dim3((unsigned)(s.tiles * a.p.n_kv_heads * QT)), dim3(256), 0, st, a);
 }
 
@@ -539,17 +824,27 @@ extern "C" int spec_paged_attention(void *hip_stream, const spec_paged_cache *ca
   a.part = (float *)d_workspace;
   a.ml = need ? a.part + (size_t)s.units * cache->n_kv_heads * s.R * cache->head_dim : nullptr;
   // without a second kernel one chunk holds everything: max_len is at most the shortest chunk
-  a.slots = std::max(1, PA_SLOTS / cache->n_kv_heads);
+  a.slots = s.slots;
   hipStream_t st = (hipStream_t)hip_stream;
+  if (s.R == PC_ROWS) {
+    const hipError_t e = allow_chunk_lds();
+    if (e != hipSuccess) return fail_noctx(SPEC_ERR_HIP, "%s: %s", who, hipGetErrorString(e));
+  }
   SPEC_DISPATCH_DTYPE(cache->dtype, T, {
     if (cache->head_dim == 64) {
       if (s.qt == 1) attend_launch<T, 64, 1>(a, s, st);
       else if (s.qt == 2) attend_launch<T, 64, 2>(a, s, st);
-      else if constexpr (sizeof(T) == 2) attend_launch<T, 64, 4>(a, s, st);
+      else if constexpr (sizeof(T) == 2) {
+        if (s.qt == 4) attend_launch<T, 64, 4>(a, s, st);
+        else attend_launch<T, 64, PC_ROWS / 16>(a, s, st);
+      }
     } else {
       if (s.qt == 1) attend_launch<T, 128, 1>(a, s, st);
       else if (s.qt == 2) attend_launch<T, 128, 2>(a, s, st);
-      else if constexpr (sizeof(T) == 2) attend_launch<T, 128, 4>(a, s, st);
+      else if constexpr (sizeof(T) == 2) {
+        if (s.qt == 4) attend_launch<T, 128, 4>(a, s, st);
+        else attend_launch<T, 128, PC_ROWS / 16>(a, s, st);
+      }
     }
   });
   const hipError_t e = hipGetLastError();
