@@ -19,6 +19,8 @@ int paged_args(const char *who, const spec_paged_cache *c, const spec_paged_batc
   const int64_t strides[3] = {c->page_stride, c->pos_stride, c->head_stride};
   for (int64_t s : strides)
     if (s < 0 || s % unit) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: cache strides must be non-negative multiples of 16 bytes", who);
+  for (int64_t s : strides)
+    if (s / unit > 0xffffffffll) return fail_noctx(SPEC_ERR_CAPACITY, "%s: a cache stride of 64 GB or more", who);
   if (c->pos_stride < c->head_dim || (c->n_kv_heads > 1 && c->head_stride < c->head_dim) || (c->n_pages > 1 && c->page_stride < c->head_dim))
     return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: a cache stride is shorter than a head", who);
   if (!c->d_k || !c->d_v || ((uintptr_t)c->d_k & 15) || ((uintptr_t)c->d_v & 15))
@@ -35,7 +37,8 @@ int paged_args(const char *who, const spec_paged_cache *c, const spec_paged_batc
       return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: max_len=%d outside 1..%d pages of %d", who, b->max_len, b->pages_stride, c->page_size);
     if (b->max_len > (1 << 30)) return fail_noctx(SPEC_ERR_CAPACITY, "%s: max_len=%d beyond 2^30", who, b->max_len);
   }
-  *out = PagedArgs{(unsigned char *)c->d_k, (unsigned char *)c->d_v, c->page_stride, c->pos_stride, c->head_stride, c->n_pages,
+  *out = PagedArgs{(unsigned char *)c->d_k, (unsigned char *)c->d_v, (uint32_t)(c->page_stride / unit), (uint32_t)(c->pos_stride / unit),
+                   (uint32_t)(c->head_stride / unit), c->n_pages,
                    __builtin_ctz(c->page_size), c->n_kv_heads, b->B, b->rows, b->max_rows, b->max_len, b->d_row_start, b->d_len, b->d_pages,
                    b->pages_stride};
   return SPEC_OK;
@@ -124,8 +127,7 @@ __global__ __launch_bounds__(256) void k_paged_append(AppendArgs a) {
     dst = a.q_out + (row * a.q_out_stride + h * HD) * sizeof(T);
   } else {
     if (page < 0) return;
-    dst = (is_v ? a.p.v : a.p.k) +
-          (page * a.p.page_stride + (pos & ((1 << a.p.page_shift) - 1)) * a.p.pos_stride + h * a.p.head_stride) * sizeof(T);
+    dst = (is_v ? a.p.v : a.p.k) + paged_row(a.p, page, pos) + ((size_t)h * a.p.head_units << 4);
   }
   const int hu = a.half / E;  // units of a rotated half
   const bool turns = !is_v && u < hu;

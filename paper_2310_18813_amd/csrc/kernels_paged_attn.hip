@@ -157,19 +157,19 @@ template <class T, int HD> struct Step {
 };
 
 template <class T, int HD>
-__device__ __forceinline__ void load_step(Step<T, HD> &f, const PagedArgs &p, int64_t head_at, int page_k, int page_v, int ks, int r, int g) {
-  constexpr int E = Step<T, HD>::E, VE = Step<T, HD>::VE, VW = Step<T, HD>::VW;
-  const int mask = (1 << p.page_shift) - 1;
+__device__ __forceinline__ void load_step(Step<T, HD> &f, const PagedArgs &p, size_t head_at, int page_k, int page_v, int ks, int r, int g) {
+  constexpr int VW = Step<T, HD>::VW;
+  const size_t pos_bytes = (size_t)p.pos_units << 4;
   // an absent page's loads go to page 0, which exists; what they bring is not used
-  const T *kr = (const T *)p.k + head_at + max(page_k, 0) * p.page_stride + ((ks + 8 * (r >> 2) + (r & 3)) & mask) * p.pos_stride + g * E;
+  const unsigned char *kr = p.k + head_at + 16 * g + paged_row(p, max(page_k, 0), ks + 8 * (r >> 2) + (r & 3));
 #pragma unroll
   for (int kk = 0; kk < Step<T, HD>::KU; ++kk) {
-    f.k0[kk] = *(const u32x4_v *)(kr + kk * 4 * E);
-    f.k1[kk] = *(const u32x4_v *)(kr + 4 * p.pos_stride + kk * 4 * E);
+    f.k0[kk] = *(const u32x4_v *)(kr + 64 * kk);
+    f.k1[kk] = *(const u32x4_v *)(kr + 4 * pos_bytes + 64 * kk);
   }
-  const T *vr = (const T *)p.v + head_at + max(page_v, 0) * p.page_stride + ((ks + 8 * g) & mask) * p.pos_stride + r * VE;
+  const unsigned char *vr = p.v + head_at + 4 * VW * r + paged_row(p, max(page_v, 0), ks + 8 * g);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) __builtin_memcpy(f.v[i], __builtin_assume_aligned(vr + i * p.pos_stride, VW * 4 < 16 ? VW * 4 : 16), VW * 4);
+  for (int i = 0; i < 8; ++i) __builtin_memcpy(f.v[i], __builtin_assume_aligned(vr + i * pos_bytes, VW * 4 < 16 ? VW * 4 : 16), VW * 4);
 }
 
 // S^T of a step: s0[i] <-> key 8g + i, s1[i] <-> key 8g + 4 + i of lane (query r, g)
@@ -261,7 +261,7 @@ __global__ __launch_bounds__(256) void k_paged_attend(AttendArgs a) {
     for (int ht = 0; ht < HT; ++ht) acc[t][ht] = (f32x4_v){0.f, 0.f, 0.f, 0.f};
   }
 
-  const int64_t head_at = hk * a.p.head_stride;
+  const size_t head_at = (size_t)hk * a.p.head_units << 4;  // bytes
   // Pages of 16 of the wave's steps at a time: lane 4j + i holds that of the i-th eight positions of step j.
   const int ks0 = k_begin + 32 * wv;
   auto pages_at = [&](int ks) {
@@ -370,7 +370,7 @@ __global__ __launch_bounds__(256) void k_paged_attend(AttendArgs a) {
       for (int key = ks; key < min(ks + 32, k_end); ++key) {
         const int page = paged_page(a.p, w.b, key);
         if (page < 0) continue;
-        const T *src = (const T *)a.p.v + head_at + page * a.p.page_stride + (key & ((1 << a.p.page_shift) - 1)) * a.p.pos_stride + 4 * VE * g;
+        const T *src = (const T *)(a.p.v + head_at + paged_row(a.p, page, key)) + 4 * VE * g;
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
           if (key > pos[t] || (a.window && key <= pos[t] - a.window)) continue;
@@ -454,32 +454,31 @@ __device__ __forceinline__ float max16(const f32x16_v &x) {
 }
 __device__ __forceinline__ float max_of_halves(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
 
-// A workgroup of four waves takes 128 query rows, 32 a wave, and walks the positions in tiles of KT = 64 (heads of 128) or 128 (of 64): 16 KB
-// of keys and 16 KB of values, in LDS in operand order, twice.  32x32x16 products: a lane owns one query (lane % 32) and half of
+// A workgroup of NW waves takes 32 NW query rows, 32 a wave, and walks the positions in tiles of KT = 16 NW (heads of 128) or 32 NW (of 64):
+// 4 NW KB of keys and as much of values, in LDS in operand order, twice.  32x32x16 products: a lane owns one query (lane % 32) and half of
 // every 16 keys, so a row's maximum takes one exchange.  Keys go straight to LDS, [key][unit of 16 bytes], a row's units exchanged by its number so
 // that reading one unit of 32 rows meets every bank; of values a thread loads 8 positions of 4 elements and turns them round on
 // the way to LDS.  The maximum follows the scores only when they have grown
 // by 2^8: weights up to 2^8 are as exact in 16 bits as weights up to 1, the sums are fp32, and most tiles then rescale nothing.
-constexpr int PC_ROWS = 128;
-constexpr int PC_LDS = 4 * 16384;
+constexpr int pc_lds(int NW) { return 4 * NW * 256 * 16; }
 
-template <class T, int HD>
-__global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendArgs a) {
-  constexpr int NC = HD / 8, KK = HD / 16, DT = HD / 32, KT = 8 * 128 / NC, VC = HD / 4, IPT = 32 / VC;
+template <class T, int HD, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
+  constexpr int R = 32 * NW, NC = HD / 8, KK = HD / 16, DT = HD / 32, KT = 256 * NW / NC, VC = HD / 4, IPT = 32 / VC, UNITS = KT * NC;
   extern __shared__ __attribute__((aligned(16))) u32x4_v pc_smem[];  // [2] keys [KT][NC], [2] values [KT / 16][DT][2][32]
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
   const int Hk = a.p.n_kv_heads, unit = blockIdx.x / Hk, hk = blockIdx.x % Hk;
   Work w;
-  if (!find_work<false>(a, PC_ROWS, unit, w)) return;
+  if (!find_work<false>(a, R, unit, w)) return;
   w = in_scalars(w);
   const PagedSeq s = w.s;
   int lo, hi;
-  tile_range(a, s, w.tile, PC_ROWS, lo, hi);
+  tile_range(a, s, w.tile, R, lo, hi);
   const int k_begin = lo + w.chunk * w.chunk_len, k_end = hi - k_begin > w.chunk_len ? k_begin + w.chunk_len : hi;
   const int rows = s.n * a.G, p0 = s.kv - s.n;
 
   // this lane's query, and what the wave's queries see: all of them [see_lo, see_hi), any of them [any_lo, any_hi)
-  const int f0 = w.tile * PC_ROWS + 32 * wv, f = f0 + col, qi = f / a.G;
+  const int f0 = w.tile * R + 32 * wv, f = f0 + col, qi = f / a.G;
   const bool on = f < rows;
   const int pos = on ? p0 + qi : -1;
   const int first = p0 + f0 / a.G, last = p0 + min(f0 + 31, rows - 1) / a.G;
@@ -492,10 +491,15 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendArgs a) {
   }
 
   // staging
-  const int vc = threadIdx.x % VC, kg = threadIdx.x / VC, mask = (1 << a.p.page_shift) - 1;
-  const int64_t head_at = hk * a.p.head_stride;
-  const T *k_base = (const T *)a.p.k + head_at, *v_base = (const T *)a.p.v + head_at + 4 * vc;
-  auto page_at = [&](int pos) { return pos < k_end ? paged_page(a.p, w.b, pos) : -1; };
+  const int vc = threadIdx.x % VC, kg = threadIdx.x / VC;
+  const size_t head_at = (size_t)hk * a.p.head_units << 4;  // bytes
+  const unsigned char *k_base = a.p.k + head_at, *v_base = a.p.v + head_at + 8 * vc;
+  const int32_t *table = a.p.pages + w.b * a.p.pages_stride;
+  const size_t pos_bytes = (size_t)a.p.pos_units << 4;
+  auto page_at = [&](int pos) {  // of a position before k_end; behind it, the last one's
+    const int page = table[(unsigned)min(pos, k_end - 1) >> a.p.page_shift];
+    return (unsigned)page < (unsigned)a.p.n_pages ? page : -1;
+  };
   // Row 32 u + 16 x + 8 y + 4 z + e of a key tile holds key 32 u + 16 x + 8 z + 4 y + e.  Wave instruction `it` fills 64 / NC rows; its
   // lanes' keys lie in one of two groups of eight positions, kgrp[it's].
   const int kgrp0 = NC == 16 ? 2 * wv : 4 * wv + (lane >> 5), kgrp1 = kgrp0 + (NC == 16 ? 1 : 2);
@@ -509,17 +513,17 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendArgs a) {
     for (int it = 0; it < 4; ++it) {
       const int key = krow + (NC == 16 ? 8 * (it & 1) + 4 * (it >> 1) : 16 * (it >> 1) + 4 * (it & 1));
       const int unit = NC == 16 ? (lane ^ (lane >> 4)) % 16 ^ 4 * it : (lane ^ (lane >> 3)) % 8;  // by the row's number
-      const T *src = k_base + max(pg.k[NC == 16 ? it & 1 : it >> 1], 0) * a.p.page_stride + ((ks + key) & mask) * a.p.pos_stride + 8 * unit;
-      lanes_to_lds(src, (unsigned)((kbuf * 1024 + (wv * 4 + it) * 64) * 16));
+      const unsigned char *src = k_base + paged_row(a.p, max(pg.k[NC == 16 ? it & 1 : it >> 1], 0), ks + key) + 16 * unit;
+      lanes_to_lds(src, (unsigned)((kbuf * UNITS + (wv * 4 + it) * 64) * 16));
     }
-    const T *src = v_base + max(pg.v, 0) * a.p.page_stride + ((ks + 8 * kg) & mask) * a.p.pos_stride;
+    const unsigned char *src = v_base + paged_row(a.p, max(pg.v, 0), ks + 8 * kg);
     x_page = pg.v;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) __builtin_memcpy(x[i], __builtin_assume_aligned(src + i * a.p.pos_stride, 8), 8);
+    for (int i = 0; i < 8; ++i) __builtin_memcpy(x[i], __builtin_assume_aligned(src + i * pos_bytes, 8), 8);
   };
   // Positions that some of the tile's rows see and others do not (those outside [all_lo, all_hi)): a weight of zero does not keep an infinity
   // or a NaN out of a product, so such values leave here and are added at the end for the rows that see them.
-  const int all_hi = p0 + w.tile * PC_ROWS / a.G + 1, all_lo = a.window ? p0 + min(w.tile * PC_ROWS + PC_ROWS - 1, rows - 1) / a.G - a.window + 1 : 0;
+  const int all_hi = p0 + w.tile * R / a.G + 1, all_lo = a.window ? p0 + min(w.tile * R + R - 1, rows - 1) / a.G - a.window + 1 : 0;
   bool odd = false;
   auto store = [&](int ks, int vbuf) {
     const int live = x_page < 0 ? 0 : k_end - (ks + 8 * kg);  // positions behind the end hold anything
@@ -531,7 +535,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) { odd |= drop_odd<T>(x[i][0]); odd |= drop_odd<T>(x[i][1]); }
     }
-    u32x4_v *vb = pc_smem + (2 + vbuf) * 1024 + (kg >> 1) * DT * 64 + (kg & 1) * 32 + vc;
+    u32x4_v *vb = pc_smem + (2 + vbuf) * UNITS + (kg >> 1) * DT * 64 + (kg & 1) * 32 + vc;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       u32x4_v y;
@@ -610,7 +614,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendArgs a) {
     fetch(ks0 + KT, pages, buf ^ 1);
     pages = pages_of(ks0 + 2 * KT);
     const int there = there_at(ks0 + KT);
-    const u32x4_v *kb = pc_smem + buf * 1024, *vb = pc_smem + (2 + buf) * 1024 + h * 32 + col;
+    const u32x4_v *kb = pc_smem + buf * UNITS, *vb = pc_smem + (2 + buf) * UNITS + h * 32 + col;
 #pragma unroll
     for (int step = 0; step < KT / 64; ++step) {
       const int ks = ks0 + 64 * step;
@@ -646,13 +650,16 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendArgs a) {
   if (lane == 0) flags[wv] = 0;
   if (odd) flags[wv] = 1;
   meet();
-  if (flags[0] | flags[1] | flags[2] | flags[3]) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) any |= flags[i];
+  if (any) {
     const int from = a.window ? pos - a.window + 1 : 0;
     for (int key = k_begin; key < k_end; ++key) {
       if (key >= all_lo && key < all_hi) { key = all_hi - 1; continue; }
       const int page = page_at(key);
       if (page < 0 || key > pos || key < from) continue;
-      const T *src = (const T *)a.p.v + head_at + page * a.p.page_stride + (key & mask) * a.p.pos_stride;
+      const T *src = (const T *)(a.p.v + head_at + paged_row(a.p, page, key));
 #pragma unroll
       for (int j = 0; j < DT; ++j)
 #pragma unroll
@@ -665,7 +672,7 @@ __global__ __launch_bounds__(256, 2) void k_paged_chunk(AttendArgs a) {
   if (!on) return;
   // element 4 c + i of the query lies in tile i / IPT, row c + VC (i % IPT); a lane holds the rows 8 (e / 4) + 4 h + e % 4
   const bool several = w.chunks > 1;
-  const int64_t at = (int64_t)blockIdx.x * PC_ROWS + 32 * wv + col;
+  const int64_t at = (int64_t)blockIdx.x * R + 32 * wv + col;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   T *dst = (T *)a.out + (s.row0 + qi) * a.out_stride + (hk * a.G + f - qi * a.G) * HD;
   if (several && h == 0) { a.ml[at * 2] = m; a.ml[at * 2 + 1] = l; }
@@ -731,11 +738,11 @@ struct Shape { int qt, R, slots; int64_t tiles, units; bool join; };
 static Shape attend_shape(const spec_paged_cache *c, const spec_paged_batch *b, int n_q) {
   Shape s;
   const int64_t G = n_q / c->n_kv_heads, per = (int64_t)b->max_rows * G;
-  s.qt = per <= 16 ? 1 : per <= 32 || c->dtype == SPEC_DTYPE_F32 ? 2 : per <= 64 ? 4 : PC_ROWS / 16;
+  s.qt = per <= 16 ? 1 : per <= 32 || c->dtype == SPEC_DTYPE_F32 ? 2 : per <= 64 ? 4 : per <= 128 ? 8 : 16;
   s.R = 16 * s.qt;
   s.tiles = std::min((int64_t)b->B * ((per + s.R - 1) / s.R), (int64_t)b->rows * G / s.R + b->B);
   s.join = b->max_len > PA_CHUNK_MIN;
-  s.slots = std::max(1, (s.R == PC_ROWS ? PC_SLOTS : PA_SLOTS) / c->n_kv_heads);
+  s.slots = std::max(1, (s.qt >= 8 ? PC_SLOTS * 8 / s.qt : PA_SLOTS) / c->n_kv_heads);
   s.units = s.tiles + (s.join ? s.slots : 0);
   return s;
 }
@@ -765,10 +772,10 @@ static hipError_t allow_chunk_lds() {
   if (e != hipSuccess) return e;
   std::lock_guard<std::mutex> lock(mutex);
   if (dev >= 0 && dev < 64 && done[dev]) return hipSuccess;
-  const void *kernels[4] = {(const void *)k_paged_chunk<bf16_t, 64>, (const void *)k_paged_chunk<bf16_t, 128>,
-                            (const void *)k_paged_chunk<f16_t, 64>, (const void *)k_paged_chunk<f16_t, 128>};
+  const void *kernels[4] = {(const void *)k_paged_chunk<bf16_t, 64, 8>, (const void *)k_paged_chunk<bf16_t, 128, 8>,
+                            (const void *)k_paged_chunk<f16_t, 64, 8>, (const void *)k_paged_chunk<f16_t, 128, 8>};
   for (const void *k : kernels) {
-    e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, PC_LDS);
+    e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, pc_lds(8));
     if (e != hipSuccess) return e;
   }
   if (dev >= 0 && dev < 64) done[dev] = true;
@@ -778,7 +785,7 @@ static hipError_t allow_chunk_lds() {
 template <class T, int HD, int QT>
 static void attend_launch(const AttendArgs &a, const Shape &s, hipStream_t st) {
   const dim3 grid((unsigned)(s.units * a.p.n_kv_heads));
-  if constexpr (QT == PC_ROWS / 16) hipLaunchKernelGGL((k_paged_chunk<T, HD>), grid, dim3(256), PC_LDS, st, a);
+  if constexpr (QT >= 8) hipLaunchKernelGGL((k_paged_chunk<T, HD, QT / 2>), grid, dim3(32 * QT), pc_lds(QT / 2), st, a);
   else hipLaunchKernelGGL((k_paged_attend<T, HD, QT>), grid, dim3(256), 0, st, a);
   if (s.join) hipLaunchKernelGGL((k_paged_join<T, HD, QT>), dim3((unsigned)(s.tiles * a.p.n_kv_heads * QT)), dim3(256), 0, st, a);
 }
@@ -826,7 +833,7 @@ extern "C" int spec_paged_attention(void *hip_stream, const spec_paged_cache *ca
   // without a second kernel one chunk holds everything: max_len is at most the shortest chunk
   a.slots = s.slots;
   hipStream_t st = (hipStream_t)hip_stream;
-  if (s.R == PC_ROWS) {
+  if (s.qt == 16) {
     const hipError_t e = allow_chunk_lds();
     if (e != hipSuccess) return fail_noctx(SPEC_ERR_HIP, "%s: %s", who, hipGetErrorString(e));
   }
@@ -836,14 +843,16 @@ extern "C" int spec_paged_attention(void *hip_stream, const spec_paged_cache *ca
       else if (s.qt == 2) attend_launch<T, 64, 2>(a, s, st);
       else if constexpr (sizeof(T) == 2) {
         if (s.qt == 4) attend_launch<T, 64, 4>(a, s, st);
-        else attend_launch<T, 64, PC_ROWS / 16>(a, s, st);
+        else if (s.qt == 8) attend_launch<T, 64, 8>(a, s, st);
+        else attend_launch<T, 64, 16>(a, s, st);
       }
     } else {
       if (s.qt == 1) attend_launch<T, 128, 1>(a, s, st);
       else if (s.qt == 2) attend_launch<T, 128, 2>(a, s, st);
       else if constexpr (sizeof(T) == 2) {
         if (s.qt == 4) attend_launch<T, 128, 4>(a, s, st);
-        else attend_launch<T, 128, PC_ROWS / 16>(a, s, st);
+        else if (s.qt == 8) attend_launch<T, 128, 8>(a, s, st);
+        else attend_launch<T, 128, 16>(a, s, st);
       }
     }
   });

@@ -8,7 +8,7 @@ namespace spec {
 // spec_paged_cache and spec_paged_batch as the kernels take them
 struct PagedArgs {
   unsigned char *k, *v;
-  int64_t page_stride, pos_stride, head_stride;  // elements
+  uint32_t page_units, pos_units, head_units;  // strides in units of 16 bytes
   int n_pages, page_shift, n_kv_heads;
   int B, rows, max_rows, max_len;
   const int32_t *row_start, *len, *pages;
@@ -35,6 +35,11 @@ __device__ __forceinline__ PagedSeq paged_seq(const PagedArgs &a, int b) {
 __device__ __forceinline__ int paged_page(const PagedArgs &a, int b, int pos) {
   const int page = a.pages[b * a.pages_stride + (pos >> a.page_shift)];
   return (unsigned)page < (unsigned)a.n_pages ? page : -1;
+}
+
+// Byte offset of a position's row of a head: two 32 x 32 + 64 bit products, whatever the sizes of the strides.
+__device__ __forceinline__ size_t paged_row(const PagedArgs &a, int page, int pos) {
+  return ((uint64_t)(uint32_t)page * a.page_units + (uint64_t)(uint32_t)(pos & ((1 << a.page_shift) - 1)) * a.pos_units) << 4;
 }
 
 // Host: checks what both entry points share and fills `out`.  No device call.
