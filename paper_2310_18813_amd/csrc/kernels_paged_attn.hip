@@ -12,8 +12,7 @@
 // positions, whole rows of a head across 16 lanes, and turns the block round in registers.
 //
 // Chunks: a sequence with more rows or positions has more work, and the host does not know the lengths.  Every wave adds the
-// batch's work up (a load and a few shuffles) and derives from it how long a chunk is: as many chunks as fill the chip's slots
-// evenly, whatever the lengths are.
+// batch's work up (a load and a few ALU instructions) and cuts it by what an even share would be, whatever the lengths are.
 #include "paged.h"
 #include <algorithm>
 #include <cmath>
@@ -30,8 +29,6 @@ typedef __attribute__((ext_vector_type(2))) float f32x2_v;
 typedef __attribute__((ext_vector_type(4))) float f32x4_v;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_v;
 
-constexpr int PA_SLOTS = 1024;    // workgroups that a pass is cut into where it is long enough
-constexpr int PC_SLOTS = 2048;    // the same for tiles of many rows
 constexpr int PA_CHUNK_MIN = 512; // positions of the shortest chunk: a shorter context is not worth a second kernel
 constexpr int PA_WAVES = 4;
 
@@ -42,84 +39,134 @@ struct AttendArgs {
   int64_t q_stride, out_stride;  // elements
   int G, window;
   float sl2;                     // scale * log2(e)
-  float *part, *ml;              // [unit * heads][R][HD], [unit * heads][R][2]
-  int slots;                     // workgroups per key head that the work is cut into
+  float *part, *ml;              // partial results of tiles that are cut: [part * heads][R][HD], [part * heads][R][2]
+  int chunk_min;
+  float one_slot;                // 1 / workgroups per key head that the work is cut into
 };
 
 // ------------------------------------------------------------------ work
-struct Work { int b, tile, chunk, chunks, base, chunk_len; PagedSeq s; };
-__device__ __forceinline__ Work in_scalars(const Work &w) {
-  auto f = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
-  return Work{f(w.b), f(w.tile), f(w.chunk), f(w.chunks), f(w.base), f(w.chunk_len), PagedSeq{f(w.s.row0), f(w.s.n), f(w.s.kv)}};
-}
+struct Work { int b, tile, chunk, chunks, chunk_len, part; PagedSeq s; };
 
-__device__ __forceinline__ int seq_tiles(const AttendArgs &a, const PagedSeq &s, int R) { return (s.n * a.G + R - 1) / R; }
-// positions that a tile of the sequence can need, at most
-__device__ __forceinline__ int seq_span(const AttendArgs &a, const PagedSeq &s, int R) {
-  if (!a.window) return s.kv;
-  return (int)min((int64_t)s.kv, (int64_t)a.window + (R - 1) / a.G + 32);
-}
-template <class V>
-__device__ __forceinline__ V wave_scan(V v) {  // inclusive
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const V t = __shfl_up(v, o, 64);
-    if ((int)(threadIdx.x & 63) >= o) v += t;
-  }
+// Sums over the lanes of a wave up to each lane, in a few ALU instructions (a shuffle goes through LDS, and every workgroup starts with this).
+template <int CTRL, int ROWS> __device__ __forceinline__ int from_lane(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int sum_to(int v) {
+  v += from_lane<0x111, 0xf>(v); v += from_lane<0x112, 0xf>(v); v += from_lane<0x114, 0xf>(v); v += from_lane<0x118, 0xf>(v);
+  v += from_lane<0x142, 0xa>(v); v += from_lane<0x143, 0xc>(v);
   return v;
 }
+template <int CTRL, int ROWS> __device__ __forceinline__ float from_lane(float v) { return __int_as_float(from_lane<CTRL, ROWS>(__float_as_int(v))); }
+__device__ __forceinline__ float sum_of(float v) {
+  v += from_lane<0x111, 0xf>(v); v += from_lane<0x112, 0xf>(v); v += from_lane<0x114, 0xf>(v); v += from_lane<0x118, 0xf>(v);
+  v += from_lane<0x142, 0xa>(v); v += from_lane<0x143, 0xc>(v);
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+__device__ __forceinline__ float max_of_halves(float v) {  // of lanes i and i ^ 32
+  const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+}
+__device__ __forceinline__ float max_of_quarters(float v) {  // of lanes i, i ^ 16, i ^ 32, i ^ 48
+  const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return max_of_halves(fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])));
+}
 
-// Unit `unit` of the pass's work: a chunk of a tile (TILES false), or a tile (TILES true; base is then its first chunk's unit).  The
-// same for the whole wave; false: there is none.
-template <bool TILES>
-__device__ __forceinline__ bool find_work(const AttendArgs &a, int R, int unit, Work &w) {
-  const int lane = threadIdx.x & 63, per = (a.p.B + 63) / 64, first = lane * per, last = min(a.p.B, first + per);
-  PagedSeq s{};
-  long long sum = 0;
-  for (int b = first; b < last; ++b) {
-    s = paged_seq(a.p, b);
-    sum += (long long)seq_tiles(a, s, R) * seq_span(a, s, R);
-  }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) sum += __shfl_xor(sum, o, 64);
-  const long long even = (sum + a.slots - 1) / a.slots;
-  const int len = max(PA_CHUNK_MIN, (int)min((even + 127) / 128 * 128, (long long)1 << 30));
-  int units = 0, tiles = 0;
-  for (int b = first; b < last; ++b) {
-    if (per > 1) s = paged_seq(a.p, b);
-    const int t = seq_tiles(a, s, R);
-    tiles += t;
-    units += t * max(1, (seq_span(a, s, R) + len - 1) / len);
-  }
-  const int units_to = wave_scan(units), tiles_to = TILES ? wave_scan(tiles) : 0;
-  const int to = TILES ? tiles_to : units_to, mine = TILES ? tiles : units;
-  const unsigned long long here = __ballot(unit >= to - mine && unit < to);
-  if (!here) return false;
-  const int src = __builtin_ctzll(here);
-  int at = __shfl(to - mine, src, 64), base = __shfl(units_to - units, src, 64);
-  for (int b = src * per; b < min(a.p.B, src * per + per); ++b) {
-    if (per > 1) {
-      s = paged_seq(a.p, b);
-    } else {
-      s.row0 = __shfl(s.row0, src, 64); s.n = __shfl(s.n, src, 64); s.kv = __shfl(s.kv, src, 64);
+// A sequence's part of the work: its tiles of R query rows, the positions that one of them can need at most, its chunks.
+struct Share { int tiles, span, chunks, len; };
+__device__ __forceinline__ Share share_of(const AttendArgs &a, const PagedSeq &s, int R) {
+  Share x;
+  x.tiles = (s.n * a.G + R - 1) / R;
+  x.span = s.kv;
+  if (a.window) x.span = (int)min((int64_t)s.kv, (int64_t)a.window + (R - 1) / a.G + 32);
+  return x;
+}
+// `even`: the positions that every workgroup would have if the work could be cut anywhere.  A tile is cut into the number of equal chunks that
+// comes nearest: so at most slots / 1.5 tiles are cut at all, into at most 4/3 slots chunks, and there are at most slots + tiles chunks.
+__device__ __forceinline__ void cut(Share &x, int even, int align) {
+  x.chunks = max(1, (x.span + even / 2) / even);
+  x.len = ((x.span + x.chunks - 1) / x.chunks + align - 1) / align * align;
+}
+__device__ __forceinline__ int even_len(const AttendArgs &a, float work) {
+  // the sum of up to 1024 roundings a lane (6e-5 of it): a little more keeps the bounds above
+  const float even = work * a.one_slot * 1.0002f;
+  return max(a.chunk_min, even < 1.e9f ? ((int)even + 128) & ~127 : 1 << 30);
+}
+
+// CUT false: unit `unit` of a pass's work, a chunk of a tile.  CUT true: the unit-th of the tiles that are cut.  part: the first of the
+// tile's partial results (its chunks' lie `tiles` apart).  False: there is none.
+template <bool CUT>
+__device__ __forceinline__ bool find_work(const AttendArgs &a, int R, int align, int unit, Work &w) {
+  const int lane = threadIdx.x & 63, B = a.p.B;
+  auto lane_of = [](int v, int l) { return __builtin_amdgcn_readlane(v, l); };
+  auto take = [&](int b, const PagedSeq &s, const Share &x, int u, int part) {
+    w.b = b; w.s = s; w.chunks = x.chunks; w.chunk_len = x.len;
+    // the last rows of a sequence see the most: their tiles start first
+    w.tile = CUT ? u : x.tiles - 1 - u % x.tiles;
+    w.chunk = CUT ? 0 : u / x.tiles;
+    w.part = part + (CUT ? u : w.tile + w.chunk * x.tiles);
+  };
+  if (B <= 64) {
+    PagedSeq s{0, 0, 0};
+    int b = lane;
+    if (lane < B) s = paged_seq(a.p, lane);
+    Share x = share_of(a, s, R);
+    if (B > 1) {  // longest first, which leaves the short ones to fill the end
+      int rank = 0;
+      for (int j = 0; j < B; ++j) {
+        const int other = lane_of(x.span, j);
+        rank += other > x.span || (other == x.span && j < lane);
+      }
+      if (lane >= B) rank = lane;
+      s.row0 = __builtin_amdgcn_ds_permute(4 * rank, s.row0);
+      s.n = __builtin_amdgcn_ds_permute(4 * rank, s.n);
+      s.kv = __builtin_amdgcn_ds_permute(4 * rank, s.kv);
+      b = __builtin_amdgcn_ds_permute(4 * rank, lane);
+      x = share_of(a, s, R);
     }
-    const int t = seq_tiles(a, s, R), c = max(1, (seq_span(a, s, R) + len - 1) / len), n = TILES ? t : t * c;
+    cut(x, even_len(a, sum_of((float)x.tiles * (float)x.span)), align);
+    const int units = CUT ? (x.chunks > 1 ? x.tiles : 0) : x.tiles * x.chunks, to = sum_to(units);
+    const int parts = x.chunks > 1 ? x.tiles * x.chunks : 0, parts_to = sum_to(parts);
+    const unsigned long long here = __ballot(unit >= to - units && unit < to);
+    if (!here) return false;
+    const int l = __builtin_ctzll(here);
+    take(lane_of(b, l), PagedSeq{lane_of(s.row0, l), lane_of(s.n, l), lane_of(s.kv, l)},
+         Share{lane_of(x.tiles, l), 0, lane_of(x.chunks, l), lane_of(x.len, l)}, unit - lane_of(to - units, l), lane_of(parts_to - parts, l));
+    return true;
+  }
+  const int per = (B + 63) / 64, first = lane * per, last = min(B, first + per);
+  float work = 0.f;
+  for (int b = first; b < last; ++b) {
+    const Share x = share_of(a, paged_seq(a.p, b), R);
+    work += (float)x.tiles * (float)x.span;
+  }
+  const int even = even_len(a, sum_of(work));
+  int units = 0, parts = 0;
+  for (int b = first; b < last; ++b) {
+    Share x = share_of(a, paged_seq(a.p, b), R);
+    cut(x, even, align);
+    units += CUT ? (x.chunks > 1 ? x.tiles : 0) : x.tiles * x.chunks;
+    parts += x.chunks > 1 ? x.tiles * x.chunks : 0;
+  }
+  const int to = sum_to(units), parts_to = sum_to(parts);
+  const unsigned long long here = __ballot(unit >= to - units && unit < to);
+  if (!here) return false;
+  const int l = __builtin_ctzll(here);
+  int at = lane_of(to - units, l), part = lane_of(parts_to - parts, l);
+  for (int b = l * per; b < min(B, l * per + per); ++b) {
+    const PagedSeq s = paged_seq(a.p, b);
+    Share x = share_of(a, s, R);
+    cut(x, even, align);
+    const int n = CUT ? (x.chunks > 1 ? x.tiles : 0) : x.tiles * x.chunks;
     if (unit < at + n) {
-      const int u = unit - at;
-      w.b = b;
-      w.chunks = c;
-      // the last rows of a sequence see the most: their tiles start first
-      w.tile = TILES ? t - 1 - u : t - 1 - u % t;
-      w.chunk = TILES ? 0 : u / t;
-      w.base = TILES ? base + u : 0;  // the tile's chunk j is unit base + j * tiles
-      w.chunk_len = len;
-      w.s = s;
+      take(b, s, x, unit - at, part);
       return true;
     }
     at += n;
-    base += t * c;
+    part += x.chunks > 1 ? x.tiles * x.chunks : 0;
   }
   return false;
+}
+__device__ __forceinline__ Work in_scalars(const Work &w) {
+  auto f = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  return Work{f(w.b), f(w.tile), f(w.chunk), f(w.chunks), f(w.chunk_len), f(w.part), PagedSeq{f(w.s.row0), f(w.s.n), f(w.s.kv)}};
 }
 
 // The positions [lo, hi) that any row of a tile sees, lo rounded down to a step.
@@ -156,20 +203,24 @@ template <class T, int HD> struct Step {
   uint32_t v[8][VW];
 };
 
+// (an absent page's loads go to page 0, which exists; what they bring is not used)
 template <class T, int HD>
-__device__ __forceinline__ void load_step(Step<T, HD> &f, const PagedArgs &p, size_t head_at, int page_k, int page_v, int ks, int r, int g) {
-  constexpr int VW = Step<T, HD>::VW;
-  const size_t pos_bytes = (size_t)p.pos_units << 4;
-  // an absent page's loads go to page 0, which exists; what they bring is not used
-  const unsigned char *kr = p.k + head_at + 16 * g + paged_row(p, max(page_k, 0), ks + 8 * (r >> 2) + (r & 3));
+__device__ __forceinline__ void load_keys(Step<T, HD> &f, const PagedArgs &p, size_t head_at, int page, int ks, int r, int g) {
+  const unsigned char *kr = p.k + head_at + 16 * g + paged_row(p, max(page, 0), ks + 8 * (r >> 2) + (r & 3));
+  const size_t four = (size_t)p.pos_units << 6;
 #pragma unroll
   for (int kk = 0; kk < Step<T, HD>::KU; ++kk) {
     f.k0[kk] = *(const u32x4_v *)(kr + 64 * kk);
-    f.k1[kk] = *(const u32x4_v *)(kr + 4 * pos_bytes + 64 * kk);
+    f.k1[kk] = *(const u32x4_v *)(kr + four + 64 * kk);
   }
-  const unsigned char *vr = p.v + head_at + 4 * VW * r + paged_row(p, max(page_v, 0), ks + 8 * g);
+}
+template <class T, int HD>
+__device__ __forceinline__ void load_values(Step<T, HD> &f, const PagedArgs &p, size_t head_at, int page, int ks, int r, int g) {
+  constexpr int VW = Step<T, HD>::VW;
+  const unsigned char *vr = p.v + head_at + 4 * VW * r + paged_row(p, max(page, 0), ks + 8 * g);
+  const size_t one = (size_t)p.pos_units << 4;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) __builtin_memcpy(f.v[i], __builtin_assume_aligned(vr + i * pos_bytes, VW * 4 < 16 ? VW * 4 : 16), VW * 4);
+  for (int i = 0; i < 8; ++i) __builtin_memcpy(f.v[i], __builtin_assume_aligned(vr + i * one, VW * 4 < 16 ? VW * 4 : 16), VW * 4);
 }
 
 // S^T of a step: s0[i] <-> key 8g + i, s1[i] <-> key 8g + 4 + i of lane (query r, g)
@@ -218,17 +269,21 @@ template <class T> __device__ __forceinline__ float only_odd(T t) {
 }
 
 // ------------------------------------------------------------------ few query rows a tile: the waves share the positions
+// Workgroups that a CU holds at a time: by registers, which its launch bound holds the compiler to.
+constexpr int attend_resident(int dtype_bytes, int HD, int QT) {
+  if (dtype_bytes == 4) return HD == 64 && QT == 1 ? 3 : HD == 64 ? 2 : 1;
+  return QT == 1 ? (HD == 64 ? 4 : 3) : QT == 2 ? (HD == 64 ? 3 : 2) : QT == 4 ? 1 : QT == 8 ? 2 : 1;
+}
 template <class T, int HD, int QT>
-__global__ __launch_bounds__(256) void k_paged_attend(AttendArgs a) {
+__global__ __launch_bounds__(256, attend_resident(sizeof(T), HD, QT)) void k_paged_attend(AttendArgs a) {
   typedef Step<T, HD> St;
   constexpr int R = 16 * QT, HT = HD / 16, KU = St::KU, VE = St::VE, LD = HD + 4;
-  constexpr bool AHEAD = QT * HD * (int)sizeof(T) < 1024;  // registers for the next step's loads beside this step's
   __shared__ float sh_o[PA_WAVES][16][LD];
   __shared__ float sh_m[PA_WAVES][R], sh_l[PA_WAVES][R];
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int Hk = a.p.n_kv_heads, unit = blockIdx.x / Hk, hk = blockIdx.x % Hk;
   Work w;
-  if (!find_work<false>(a, R, unit, w)) return;
+  if (!find_work<false>(a, R, 128, unit, w)) return;
   w = in_scalars(w);
   const PagedSeq s = w.s;
   int lo, hi;
@@ -268,52 +323,39 @@ __global__ __launch_bounds__(256) void k_paged_attend(AttendArgs a) {
     const int pos = ks + 128 * (lane >> 2) + 8 * (lane & 3);
     return pos < k_end ? paged_page(a.p, w.b, pos) : -1;
   };
-  int pages = -1, pages_next = -1;
-  St cur, nxt;
-  int pk = -1, pv = -1, pk_n = -1, pv_n = -1;
+  int pages = -1, pages_next = -1, pk = -1, pv = -1, pv_next = -1;
+  St f;
   if (ks0 < k_end) {
     pages = pages_at(ks0);
     pages_next = pages_at(ks0 + 16 * 128);
     pk = __shfl(pages, r >> 2, 64);
     pv = __shfl(pages, g, 64);
-    load_step<T, HD>(cur, a.p, head_at, pk, pv, ks0, r, g);
+    load_keys<T, HD>(f, a.p, head_at, pk, ks0, r, g);
+    load_values<T, HD>(f, a.p, head_at, pv, ks0, r, g);
   }
   int j = 0;
   bool odd = false;
   for (int ks = ks0; ks < k_end; ks += 128) {
-    if (ks + 128 < k_end) {
+    const bool more = ks + 128 < k_end;
+    if (more) {
       if (++j == 16) {
         j = 0;
         pages = pages_next;
         pages_next = pages_at(ks + 128 + 16 * 128);
       }
-      pk_n = __shfl(pages, 4 * j + (r >> 2), 64);
-      pv_n = __shfl(pages, 4 * j + g, 64);
-      if (AHEAD) load_step<T, HD>(nxt, a.p, head_at, pk_n, pv_n, ks + 128, r, g);
-    }
-    // keys of this lane's scores: ks + 8g + i, in page pv
-    const bool whole = ks >= see_lo && ks + 32 <= min(see_hi, k_end) && __all(pv >= 0);
-    if (!whole) {  // positions that no row of the tile sees: their values, whatever they are, become zeros
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const bool live = pv >= 0 && ks + 8 * g + i < k_end && ks + 8 * g + i >= 0;
-#pragma unroll
-        for (int x = 0; x < St::VW; ++x) cur.v[i][x] = live ? cur.v[i][x] : 0u;
-      }
-    }
-    // Positions that some of the tile's rows see and others do not: a weight of zero does not keep an infinity or a NaN out of a
-    // product, so such values leave here and are added at the end for the rows that see them.
-    if (!whole && i0 != i1) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int x = 0; x < St::VW; ++x) odd |= drop_odd<T>(cur.v[i][x]);
+      pk = __shfl(pages, 4 * j + (r >> 2), 64);
+      pv_next = __shfl(pages, 4 * j + g, 64);
     }
     float p[QT][8];
 #pragma unroll
+    for (int t = 0; t < QT; ++t) scores<T, HD>(f, q[t], p[t]);
+    // the keys are used: the next step's take their registers while the weights are worked out, and the next values' these values'
+    if (more) load_keys<T, HD>(f, a.p, head_at, pk, ks + 128, r, g);
+    // keys of this lane's scores: ks + 8g + i, in page pv
+    const bool whole = ks >= see_lo && ks + 32 <= min(see_hi, k_end) && __all(pv >= 0);
+#pragma unroll
     for (int t = 0; t < QT; ++t) {
-      float sv[8];
-      scores<T, HD>(cur, q[t], sv);
+      float(&sv)[8] = p[t];
       if (!whole) {
         const int from = a.window ? pos[t] - a.window + 1 : 0;
 #pragma unroll
@@ -322,9 +364,7 @@ __global__ __launch_bounds__(256) void k_paged_attend(AttendArgs a) {
           sv[i] = pv >= 0 && key <= pos[t] && key >= from && key < k_end ? sv[i] : -INFINITY;
         }
       }
-      float top = fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])), fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
-      top = fmaxf(top, __shfl_xor(top, 16, 64));
-      top = fmaxf(top, __shfl_xor(top, 32, 64));
+      const float top = max_of_quarters(fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])), fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7]))));
       if (__any(top > m[t])) {
         const float mn = fmaxf(m[t], top);
         const float corr = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[t] - mn) * a.sl2);
@@ -336,32 +376,49 @@ __global__ __launch_bounds__(256) void k_paged_attend(AttendArgs a) {
       const float off = m[t] == -INFINITY ? 0.f : m[t] * a.sl2;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        p[t][i] = __builtin_amdgcn_exp2f(fmaf(sv[i], a.sl2, -off));
-        l[t] += p[t][i];
+        sv[i] = __builtin_amdgcn_exp2f(fmaf(sv[i], a.sl2, -off));
+        l[t] += sv[i];
       }
+    }
+    if (!whole) {  // positions that no row of the tile sees: their values, whatever they are, become zeros
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const bool live = pv >= 0 && ks + 8 * g + i < k_end;
+#pragma unroll
+        for (int x = 0; x < St::VW; ++x) f.v[i][x] = live ? f.v[i][x] : 0u;
+      }
+      // Positions that some of the tile's rows see and others do not: a weight of zero does not keep an infinity or a NaN out of a
+      // product, so such values leave here and are added at the end for the rows that see them.
+      if (i0 != i1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int x = 0; x < St::VW; ++x) odd |= drop_odd<T>(f.v[i][x]);
+      }
+    }
+    u32x4_v y[QT];
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) y[t][d] = Mat<T>::pack2(p[t][2 * d], p[t][2 * d + 1]);
     }
 #pragma unroll
     for (int ht = 0; ht < HT; ++ht) {
       if constexpr (sizeof(T) == 2) {
-        const u32x4_v x = value_operand<T, HD>(cur, ht);
+        const u32x4_v x = value_operand<T, HD>(f, ht);
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-          u32x4_v y;
-#pragma unroll
-          for (int d = 0; d < 4; ++d) y[d] = Mat<T>::pack2(p[t][2 * d], p[t][2 * d + 1]);
-          acc[t][ht] = Mat<T>::run(x, y, acc[t][ht]);
-        }
+        for (int t = 0; t < QT; ++t) acc[t][ht] = Mat<T>::run(x, y[t], acc[t][ht]);
       } else {
 #pragma unroll
         for (int t = 0; t < QT; ++t)
 #pragma unroll
           for (int i = 0; i < 8; ++i)
-            acc[t][ht] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(cur.v[i][ht]), p[t][i], acc[t][ht], 0, 0, 0);
+            acc[t][ht] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(f.v[i][ht]), p[t][i], acc[t][ht], 0, 0, 0);
       }
     }
-    if (AHEAD) cur = nxt;
-    else if (ks + 128 < k_end) load_step<T, HD>(cur, a.p, head_at, pk_n, pv_n, ks + 128, r, g);
-    pv = pv_n;
+    if (more) load_values<T, HD>(f, a.p, head_at, pv_next, ks + 128, r, g);
+    pv = pv_next;
   }
 
   if (__any(odd)) {  // this wave's steps of the positions outside [see_lo, see_hi) again
@@ -391,7 +448,7 @@ __global__ __launch_bounds__(256) void k_paged_attend(AttendArgs a) {
     if (g == 0) { sh_m[wv][16 * t + r] = m[t]; sh_l[wv][16 * t + r] = l[t]; }
   }
   __syncthreads();
-  const int64_t slot = (int64_t)blockIdx.x * R;
+  const int64_t slot = ((int64_t)w.part * Hk + hk) * R;
 #pragma unroll
   for (int t = 0; t < QT; ++t) {
     float mt = -INFINITY;
@@ -452,7 +509,6 @@ __device__ __forceinline__ float max16(const f32x16_v &x) {
         "v"(x[12]), "v"(x[13]), "v"(x[14]), "v"(x[15]));
   return r;
 }
-__device__ __forceinline__ float max_of_halves(float v) { return fmaxf(v, __shfl_xor(v, 32, 64)); }
 
 // A workgroup of NW waves takes 32 NW query rows, 32 a wave, and walks the positions in tiles of KT = 16 NW (heads of 128) or 32 NW (of 64):
 // 4 NW KB of keys and as much of values, in LDS in operand order, twice.  32x32x16 products: a lane owns one query (lane % 32) and half of
@@ -469,7 +525,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, h = lane >> 5;
   const int Hk = a.p.n_kv_heads, unit = blockIdx.x / Hk, hk = blockIdx.x % Hk;
   Work w;
-  if (!find_work<false>(a, R, unit, w)) return;
+  if (!find_work<false>(a, R, KT, unit, w)) return;
   w = in_scalars(w);
   const PagedSeq s = w.s;
   int lo, hi;
@@ -672,7 +728,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
   if (!on) return;
   // element 4 c + i of the query lies in tile i / IPT, row c + VC (i % IPT); a lane holds the rows 8 (e / 4) + 4 h + e % 4
   const bool several = w.chunks > 1;
-  const int64_t at = (int64_t)blockIdx.x * R + 32 * wv + col;
+  const int64_t at = ((int64_t)w.part * Hk + hk) * R + 32 * wv + col;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   T *dst = (T *)a.out + (s.row0 + qi) * a.out_stride + (hk * a.G + f - qi * a.G) * HD;
   if (several && h == 0) { a.ml[at * 2] = m; a.ml[at * 2 + 1] = l; }
@@ -699,30 +755,48 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
   }
 }
 
-// Joins the chunks of a tile: a workgroup takes 16 query rows of a tile, a thread VE elements of one.
+// Joins the chunks of the tiles that are cut: a workgroup takes 16 query rows of one, a thread VE elements of a row.
 template <class T, int HD, int QT>
-__global__ __launch_bounds__(256) void k_paged_join(AttendArgs a) {
-  constexpr int R = 16 * QT, VE = HD / 16;
-  const int Hk = a.p.n_kv_heads, id = blockIdx.x / QT, t = blockIdx.x % QT, unit = id / Hk, hk = id % Hk;
+__global__ __launch_bounds__(256) void k_paged_join(AttendArgs a, int align) {
+  constexpr int R = 16 * QT, VE = HD / 16, AHEAD = 8;
+  const int Hk = a.p.n_kv_heads, t = blockIdx.x % QT, unit = blockIdx.x / QT / Hk, hk = blockIdx.x / QT % Hk;
   Work w;
-  if (!find_work<true>(a, R, unit, w) || w.chunks < 2) return;
+  if (!find_work<true>(a, R, align, unit, w)) return;
+  w = in_scalars(w);
   const PagedSeq s = w.s;
   const int row = threadIdx.x >> 4, d0 = VE * (threadIdx.x & 15), f = w.tile * R + 16 * t + row;
   if (f >= s.n * a.G) return;
-  const int tiles = seq_tiles(a, s, R);
+  const int64_t next = (int64_t)((s.n * a.G + R - 1) / R) * Hk * R, at = ((int64_t)w.part * Hk + hk) * R + 16 * t + row;
+  const float2 *ml = (const float2 *)a.ml + at;
+  const float *part = a.part + at * HD + d0;
   float m = -INFINITY, l = 0.f, o[VE];
+  for (int c0 = 0; c0 < w.chunks; c0 += AHEAD) {
+    float mc[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) mc[i] = ml[min(c0 + i, w.chunks - 1) * next].x;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) m = fmaxf(m, mc[i]);
+  }
 #pragma unroll
   for (int d = 0; d < VE; ++d) o[d] = 0.f;
-  for (int c = 0; c < w.chunks; ++c) {
-    const int64_t at = ((int64_t)(w.base + c * tiles) * Hk + hk) * R + 16 * t + row;
-    const float mc = a.ml[at * 2], lc = a.ml[at * 2 + 1];
-    const float mn = fmaxf(m, mc);
-    const float wa = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * a.sl2);
-    const float wb = mc == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mc - mn) * a.sl2);
-    l = l * wa + lc * wb;
+  for (int c0 = 0; c0 < w.chunks; c0 += AHEAD) {
+    float2 x[AHEAD];
+    f32x4_v y[AHEAD][VE / 4];
 #pragma unroll
-    for (int d = 0; d < VE; ++d) o[d] = o[d] * wa + a.part[at * HD + d0 + d] * wb;
-    m = mn;
+    for (int i = 0; i < AHEAD; ++i) {
+      const int64_t c = min(c0 + i, w.chunks - 1) * next;
+      x[i] = ml[c];
+#pragma unroll
+      for (int d = 0; d < VE / 4; ++d) y[i][d] = *(const f32x4_v *)(part + c * HD + 4 * d);
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (c0 + i >= w.chunks) break;
+      const float wt = x[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[i].x - m) * a.sl2);
+      l += x[i].y * wt;
+#pragma unroll
+      for (int d = 0; d < VE; ++d) o[d] += y[i][d / 4][d % 4] * wt;
+    }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int i = f / a.G;
@@ -732,22 +806,31 @@ __global__ __launch_bounds__(256) void k_paged_join(AttendArgs a) {
 }
 
 // ------------------------------------------------------------------ launch
-struct Shape { int qt, R, slots; int64_t tiles, units; bool join; };
+struct Shape {
+  int qt, R, align, slots;             // slots: workgroups per key head that fill the chip
+  int64_t tiles, units, cut, parts;    // per key head, at most: tiles, chunks, tiles that are cut, their chunks
+};
 
-// Query rows of a tile: as few as hold a sequence's, since a tile reads the cache once for all of its rows.
+// Query rows of a tile: as few as hold a sequence's, since a tile reads the cache once for all of its rows.  Beyond 64 rows 128, or 256
+// where there are enough tiles of those.
 static Shape attend_shape(const spec_paged_cache *c, const spec_paged_batch *b, int n_q) {
-  Shape s;
-  const int64_t G = n_q / c->n_kv_heads, per = (int64_t)b->max_rows * G;
-  s.qt = per <= 16 ? 1 : per <= 32 || c->dtype == SPEC_DTYPE_F32 ? 2 : per <= 64 ? 4 : per <= 128 ? 8 : 16;
+  Shape s{};
+  const int64_t Hk = c->n_kv_heads, G = n_q / Hk, per = (int64_t)b->max_rows * G;
+  auto tiles = [&](int R) { return std::min((int64_t)b->B * ((per + R - 1) / R), (int64_t)b->rows * G / R + b->B); };
+  const bool f32 = c->dtype == SPEC_DTYPE_F32;
+  s.qt = per <= 16 && !(f32 && c->head_dim == 128) ? 1 : per <= 32 || f32 ? 2 : per <= 64 ? 4 : tiles(256) * Hk < 512 ? 8 : 16;
   s.R = 16 * s.qt;
-  s.tiles = std::min((int64_t)b->B * ((per + s.R - 1) / s.R), (int64_t)b->rows * G / s.R + b->B);
-  s.join = b->max_len > PA_CHUNK_MIN;
-  s.slots = std::max(1, (s.qt >= 8 ? PC_SLOTS * 8 / s.qt : PA_SLOTS) / c->n_kv_heads);
-  s.units = s.tiles + (s.join ? s.slots : 0);
+  s.align = s.qt < 8 ? 128 : s.R * 64 / c->head_dim;
+  s.tiles = tiles(s.R);
+  s.slots = std::max(1, 256 * attend_resident((int)dtype_bytes(c->dtype), c->head_dim, s.qt) / (int)Hk);
+  const bool one = b->max_len <= PA_CHUNK_MIN;  // one chunk holds everything
+  s.units = s.tiles + (one ? 0 : s.slots);
+  s.cut = one ? 0 : std::min<int64_t>(s.tiles, s.slots * 2 / 3 + 1);
+  s.parts = one ? 0 : s.slots * 4 / 3 + 2;
   return s;
 }
 static size_t attend_bytes(const spec_paged_cache *c, const Shape &s) {
-  return s.join ? (size_t)s.units * c->n_kv_heads * s.R * (c->head_dim + 2) * sizeof(float) : 0;
+  return (size_t)s.parts * c->n_kv_heads * s.R * (c->head_dim + 2) * sizeof(float);
 }
 static int attend_check(const char *who, const spec_paged_cache *c, const spec_paged_batch *b, int n_q, AttendArgs &a, Shape &s) {
   int rc = paged_args(who, c, b, &a.p);
@@ -756,9 +839,9 @@ static int attend_check(const char *who, const spec_paged_cache *c, const spec_p
     return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: n_q_heads=%d is not a multiple of n_kv_heads=%d", who, n_q, c->n_kv_heads);
   a.G = n_q / c->n_kv_heads;
   if ((int64_t)b->rows * a.G >= 1 << 30) return fail_noctx(SPEC_ERR_CAPACITY, "%s: more than 2^30 query rows of a key head", who);
-  if (b->B == 0 || b->rows == 0) { s = Shape{1, 16, 1, 0, 0, false}; return SPEC_OK; }
+  if (b->B == 0 || b->rows == 0) { s = Shape{};  return SPEC_OK; }
   s = attend_shape(c, b, n_q);
-  if (s.units * c->n_kv_heads * 256 >= (int64_t)1 << 32 || s.tiles * c->n_kv_heads * s.qt * 256 >= (int64_t)1 << 32)
+  if (s.units * c->n_kv_heads * 512 >= (int64_t)1 << 32)
     return fail_noctx(SPEC_ERR_CAPACITY, "%s: %lld tiles of %d key heads are beyond one launch", who, (long long)s.units, c->n_kv_heads);
   return SPEC_OK;
 }
@@ -787,7 +870,7 @@ static void attend_launch(const AttendArgs &a, const Shape &s, hipStream_t st) {
   const dim3 grid((unsigned)(s.units * a.p.n_kv_heads));
   if constexpr (QT >= 8) hipLaunchKernelGGL((k_paged_chunk<T, HD, QT / 2>), grid, dim3(32 * QT), pc_lds(QT / 2), st, a);
   else hipLaunchKernelGGL((k_paged_attend<T, HD, QT>), grid, dim3(256), 0, st, a);
-  if (s.join) hipLaunchKernelGGL((k_paged_join<T, HD, QT>), dim3((unsigned)(s.tiles * a.p.n_kv_heads * QT)), dim3(256), 0, st, a);
+  if (s.cut) hipLaunchKernelGGL((k_paged_join<T, HD, QT>), dim3((unsigned)(s.cut * a.p.n_kv_heads * QT)), dim3(256), 0, st, a, s.align);
 }
 
 }  // namespace spec
@@ -829,9 +912,9 @@ extern "C" int spec_paged_attention(void *hip_stream, const spec_paged_cache *ca
   a.window = window;
   a.sl2 = scale * 1.4426950408889634f;
   a.part = (float *)d_workspace;
-  a.ml = need ? a.part + (size_t)s.units * cache->n_kv_heads * s.R * cache->head_dim : nullptr;
-  // without a second kernel one chunk holds everything: max_len is at most the shortest chunk
-  a.slots = s.slots;
+  a.ml = need ? a.part + (size_t)s.parts * cache->n_kv_heads * s.R * cache->head_dim : nullptr;
+  a.chunk_min = PA_CHUNK_MIN;
+  a.one_slot = 1.f / s.slots;
   hipStream_t st = (hipStream_t)hip_stream;
   if (s.qt == 16) {
     const hipError_t e = allow_chunk_lds();
@@ -847,8 +930,9 @@ extern "C" int spec_paged_attention(void *hip_stream, const spec_paged_cache *ca
         else attend_launch<T, 64, 16>(a, s, st);
       }
     } else {
-      if (s.qt == 1) attend_launch<T, 128, 1>(a, s, st);
-      else if (s.qt == 2) attend_launch<T, 128, 2>(a, s, st);
+      if (s.qt == 1) {
+        if constexpr (sizeof(T) == 2) attend_launch<T, 128, 1>(a, s, st);
+      } else if (s.qt == 2) attend_launch<T, 128, 2>(a, s, st);
       else if constexpr (sizeof(T) == 2) {
         if (s.qt == 4) attend_launch<T, 128, 4>(a, s, st);
         else if (s.qt == 8) attend_launch<T, 128, 8>(a, s, st);
