@@ -269,24 +269,26 @@ class LogitRules:
         self.mask_words = None if mask is None else mask.shape[2]
         self.desc = LogitRulesDesc(p(tokens), stride, p(prompt_len), p(length), p(repetition), p(frequency), p(presence), p(bias_ids), p(bias),
                                    0 if bias is None else bias.shape[1], p(mask), 0 if mask is None else mask.shape[1])
+        self.ref = C.byref(self.desc)
 
 
 def spec_process_logits(logits, rules, proposals=None, out=None):
     """logits [B][s+1][V] (fp32, bf16 or fp16, rows may be padded), proposals [B][s] int32 or None -> out [B][s+1][V] fp32, which
     may be logits itself."""
-    assert logits.dim() == 3 and logits.dtype in _DTYPE_OF
-    nB, q, V = logits.shape
-    row = logits.stride(1) if q > 1 else logits.stride(0) if nB > 1 else V
-    assert logits.stride(2) == 1 and (nB < 2 or logits.stride(0) == q * row)
+    shape = nB, q, V = logits.shape
+    s0, s1, s2 = logits.stride()
+    row = s1 if q > 1 else s0 if nB > 1 else V
+    assert s2 == 1 and (nB < 2 or s0 == q * row)
     assert rules.B is None or rules.B == nB
     assert rules.mask_words is None or rules.mask_words == (V + 31) // 32
+    pp = None
     if proposals is not None:
-        assert proposals.dtype == torch.int32 and proposals.shape == (nB, q - 1) and proposals.is_contiguous()
+        assert proposals.dtype is torch.int32 and proposals.shape == (nB, q - 1) and proposals.is_contiguous()
+        pp = proposals.data_ptr() or None
     if out is None:
-        out = torch.empty((nB, q, V), dtype=torch.float32, device=logits.device)
-    assert out.dtype == torch.float32 and out.shape == (nB, q, V) and out.is_contiguous()
-    _call(logits.device, lib.spec_process_logits, logits.data_ptr(), _DTYPE_OF[logits.dtype], row, nB, q - 1, V, C.byref(rules.desc),
-          proposals.data_ptr() if proposals is not None and q > 1 else None, out.data_ptr())
+        out = torch.empty(shape, dtype=torch.float32, device=logits.device)
+    assert out.dtype is torch.float32 and out.shape == shape and out.is_contiguous()
+    _call(logits.device, lib.spec_process_logits, logits.data_ptr(), _DTYPE_OF[logits.dtype], row, nB, q - 1, V, rules.ref, pp, out.data_ptr())
     return out
 
 
@@ -302,7 +304,9 @@ class PagedCache:
         assert k.stride() == v.stride() and k.stride(3) == 1
         self.k, self.v, self.device = k, v, k.device  # the tensors must outlive their use
         n, size, heads, hd = k.shape
+        self.dtype, self.n_kv_heads, self.page_size, self.head_dim = k.dtype, heads, size, hd
         self.desc = PagedCacheDesc(_DTYPE_OF[k.dtype], hd, heads, size, n, k.stride(0), k.stride(1), k.stride(2), k.data_ptr(), v.data_ptr())
+        self.ref, self.scale = C.byref(self.desc), hd ** -0.5
 
 
 class PagedBatch:
@@ -316,25 +320,31 @@ class PagedBatch:
         assert lengths.dim() == 1 and lengths.dtype == torch.int32 and lengths.is_contiguous()
         assert row_start is None or (row_start.dtype == torch.int32 and row_start.shape == (nB + 1,) and row_start.is_contiguous())
         self.pages, self.lengths, self.row_start = pages, lengths, row_start  # must outlive their use
-        self.rows, self.max_rows, self.max_len = rows, max_rows, max_len
+        self.rows, self.max_len = rows, max_len
         stride = pages.stride(0) if nB > 1 else pages.shape[1]
         if max_rows is None:
             max_rows = rows if row_start is not None else max(1, rows // max(1, nB))
         self.desc = PagedBatchDesc(nB, rows, max_rows, max_len or 0, None if row_start is None else row_start.data_ptr(), lengths.data_ptr(),
                                    pages.data_ptr(), stride)
+        self.ref, self._page_size = C.byref(self.desc), None
 
     def _for(self, cache):
-        if self.max_len is None:
-            self.desc.max_len = self.pages.shape[1] * cache.desc.page_size
-        else:
-            assert self.max_len <= self.pages.shape[1] * cache.desc.page_size
-        return C.byref(self.desc)
+        if cache.page_size != self._page_size:
+            most = self.pages.shape[1] * cache.page_size
+            assert self.max_len is None or self.max_len <= most
+            self.desc.max_len = most if self.max_len is None else self.max_len
+            self._page_size = cache.page_size
+        return self.ref
 
 
-def _heads(t, rows, hd, cache):
-    assert t.dim() == 3 and t.shape[0] == rows and t.shape[2] == hd and _DTYPE_OF.get(t.dtype) == cache.desc.dtype and t.device == cache.device
-    assert t.stride(2) == 1 and (t.shape[1] < 2 or t.stride(1) == hd)
-    return t.data_ptr(), (t.stride(0) if rows > 1 else t.shape[1] * hd)
+# (the calls below are made once a layer of every round: what they check is read from a tensor once, 1 us of a call each)
+def _heads(t, rows, cache):
+    """-> (address, row stride, heads) of a row-wise tensor [rows][heads][head_dim]."""
+    n, heads, hd = t.shape
+    s0, s1, s2 = t.stride()
+    assert n == rows and hd == cache.head_dim and t.dtype is cache.dtype and t.get_device() == cache.device.index
+    assert s2 == 1 and (s1 == hd or heads < 2)
+    return t.data_ptr(), (s0 if rows > 1 else heads * hd), heads
 
 
 def spec_rope_frequencies(theta, rope_dim, device="cuda:0"):
@@ -345,49 +355,45 @@ def spec_rope_frequencies(theta, rope_dim, device="cuda:0"):
 def spec_paged_append(cache, batch, q, k, v, inv_freq=None, out=None):
     """k, v [rows][n_kv_heads][head_dim] into the pages; q [rows][n_q_heads][head_dim] (None: keys and values only) and k rotated by
     position * inv_freq (float64 [rope_dim / 2], None: no rotation).  -> out, the rotated q (may be q itself); None without q."""
-    d = cache.desc
     rows = batch.rows
-    kp, ks = _heads(k, rows, d.head_dim, cache)
-    vp, vs = _heads(v, rows, d.head_dim, cache)
-    assert k.shape[1] == v.shape[1] == d.n_kv_heads
+    kp, ks, kh = _heads(k, rows, cache)
+    vp, vs, vh = _heads(v, rows, cache)
+    assert kh == vh == cache.n_kv_heads
     qp = op = None
     qs = os_ = nq = 0
     if q is not None:
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        assert out.shape == q.shape
-        nq = q.shape[1]
-        qp, qs = _heads(q, rows, d.head_dim, cache)
-        op, os_ = _heads(out, rows, d.head_dim, cache)
-    rope = 0
+        qp, qs, nq = _heads(q, rows, cache)
+        op, os_, no = _heads(out, rows, cache)
+        assert no == nq
+    rope, fp = 0, None
     if inv_freq is not None:
-        assert inv_freq.dtype == torch.float64 and inv_freq.dim() == 1 and inv_freq.is_contiguous() and inv_freq.device == cache.device
-        rope = 2 * inv_freq.shape[0]
-    _call(cache.device, lib.spec_paged_append, C.byref(d), batch._for(cache), nq, qp, qs, kp, ks, vp, vs,
-          inv_freq.data_ptr() if rope else None, rope, op, os_)
+        assert inv_freq.dtype is torch.float64 and inv_freq.dim() == 1 and inv_freq.is_contiguous() and inv_freq.get_device() == cache.device.index
+        rope, fp = 2 * inv_freq.shape[0], inv_freq.data_ptr()
+    _call(cache.device, lib.spec_paged_append, cache.ref, batch._for(cache), nq, qp, qs, kp, ks, vp, vs, fp, rope, op, os_)
     return out if q is not None else None
 
 
 def spec_paged_attention_workspace_bytes(cache, batch, n_q_heads):
     n = C.c_size_t(0)
-    _check(lib.spec_paged_attention_workspace_bytes(C.byref(cache.desc), batch._for(cache), n_q_heads, C.byref(n)))
+    _check(lib.spec_paged_attention_workspace_bytes(cache.ref, batch._for(cache), n_q_heads, C.byref(n)))
     return n.value
 
 
 def spec_paged_attention(cache, batch, q, scale=None, window=0, out=None, workspace=None):
     """q [rows][n_q_heads][head_dim] over the pages -> out, the same shape.  scale: 1 / sqrt(head_dim) if None.  workspace: a uint8
     tensor of spec_paged_attention_workspace_bytes() (allocated if None)."""
-    d = cache.desc
-    rows, nq = batch.rows, q.shape[1]
+    rows = batch.rows
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    assert out.shape == q.shape
-    qp, qs = _heads(q, rows, d.head_dim, cache)
-    op, os_ = _heads(out, rows, d.head_dim, cache)
+    qp, qs, nq = _heads(q, rows, cache)
+    op, os_, no = _heads(out, rows, cache)
+    assert no == nq
     if workspace is None:
         workspace = torch.empty(spec_paged_attention_workspace_bytes(cache, batch, nq), dtype=torch.uint8, device=q.device)
-    _call(cache.device, lib.spec_paged_attention, C.byref(d), batch._for(cache), nq, qp, qs, d.head_dim ** -0.5 if scale is None else float(scale),
-          int(window), workspace.data_ptr() if workspace.numel() else None, workspace.numel(), op, os_)
+    _call(cache.device, lib.spec_paged_attention, cache.ref, batch._for(cache), nq, qp, qs, cache.scale if scale is None else scale, window,
+          workspace.data_ptr() or None, workspace.numel(), op, os_)
     return out
 
 
