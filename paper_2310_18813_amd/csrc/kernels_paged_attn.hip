@@ -29,7 +29,7 @@ typedef __attribute__((ext_vector_type(2))) float f32x2_v;
 typedef __attribute__((ext_vector_type(4))) float f32x4_v;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_v;
 
-constexpr int PA_CHUNK_MIN = 512; // positions of the shortest chunk: a shorter context is not worth a second kernel
+constexpr int PA_CHUNK_MIN = 512; // positions of the shortest chunk
 constexpr int PA_WAVES = 4;
 
 struct AttendArgs {
@@ -203,10 +203,10 @@ template <class T, int HD> struct Step {
   uint32_t v[8][VW];
 };
 
-// (an absent page's loads go to page 0, which exists; what they bring is not used)
+// (an absent page's loads are sent to page 0, which exists; what they bring is not used)
 template <class T, int HD>
 __device__ __forceinline__ void load_keys(Step<T, HD> &f, const PagedArgs &p, size_t head_at, int page, int ks, int r, int g) {
-  const unsigned char *kr = p.k + head_at + 16 * g + paged_row(p, max(page, 0), ks + 8 * (r >> 2) + (r & 3));
+  const unsigned char *kr = p.k + head_at + 16 * g + paged_row(p, page, ks + 8 * (r >> 2) + (r & 3));
   const size_t four = (size_t)p.pos_units << 6;
 #pragma unroll
   for (int kk = 0; kk < Step<T, HD>::KU; ++kk) {
@@ -217,7 +217,7 @@ __device__ __forceinline__ void load_keys(Step<T, HD> &f, const PagedArgs &p, si
 template <class T, int HD>
 __device__ __forceinline__ void load_values(Step<T, HD> &f, const PagedArgs &p, size_t head_at, int page, int ks, int r, int g) {
   constexpr int VW = Step<T, HD>::VW;
-  const unsigned char *vr = p.v + head_at + 4 * VW * r + paged_row(p, max(page, 0), ks + 8 * g);
+  const unsigned char *vr = p.v + head_at + 4 * VW * r + paged_row(p, page, ks + 8 * g);
   const size_t one = (size_t)p.pos_units << 4;
 #pragma unroll
   for (int i = 0; i < 8; ++i) __builtin_memcpy(f.v[i], __builtin_assume_aligned(vr + i * one, VW * 4 < 16 ? VW * 4 : 16), VW * 4);
@@ -254,13 +254,15 @@ __device__ __forceinline__ u32x4_v value_operand(const Step<T, HD> &f, int ht) {
   return x;
 }
 
-// Takes infinities and NaN out of a word of cached values; whether there were any.
-template <class T> __device__ __forceinline__ bool drop_odd(uint32_t &w) {
-  constexpr uint32_t e = sizeof(T) == 4 ? 0x7f800000u : std::is_same<T, bf16_t>::value ? 0x7f80u : 0x7c00u;
-  const bool lo = (w & e) == e, hi = sizeof(T) == 2 && (w >> 16 & e) == e;
-  if (sizeof(T) == 4) w = lo ? 0u : w;
-  else w &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
-  return lo || hi;
+// Takes infinities and NaN out of a word of cached values; not zero if there were any.  (In integers: as conditions, a step's would fill the scalar
+// registers.)
+template <class T> __device__ __forceinline__ uint32_t drop_odd(uint32_t &w) {
+  constexpr int top = sizeof(T) == 4 ? 31 : 15;  // of a value; two lie in a word of 16-bit ones
+  constexpr uint32_t e = top == 31 ? 0x7f800000u : std::is_same<T, bf16_t>::value ? 0x7f807f80u : 0x7c007c00u, low = top == 31 ? 0x7fffffffu : 0x7fff7fffu;
+  const uint32_t finite = (((w & e) ^ e) + low) & ~low;  // a value's top bit, where its exponent is not all ones
+  const uint32_t keep = (finite - (finite >> top)) | finite;
+  w &= keep;
+  return ~keep;
 }
 // The value if it is infinite or NaN, else zero.
 template <class T> __device__ __forceinline__ float only_odd(T t) {
@@ -272,7 +274,7 @@ template <class T> __device__ __forceinline__ float only_odd(T t) {
 // Workgroups that a CU holds at a time: by registers, which its launch bound holds the compiler to.
 constexpr int attend_resident(int dtype_bytes, int HD, int QT) {
   if (dtype_bytes == 4) return HD == 64 && QT == 1 ? 3 : HD == 64 ? 2 : 1;
-  return QT == 1 ? (HD == 64 ? 4 : 3) : QT == 2 ? (HD == 64 ? 3 : 2) : QT == 4 ? 1 : QT == 8 ? 2 : 1;
+  return QT == 1 ? (HD == 64 ? 4 : 3) : QT == 2 ? (HD == 64 ? 3 : 1) : QT == 4 ? 1 : QT == 8 ? 2 : 1;
 }
 template <class T, int HD, int QT>
 __global__ __launch_bounds__(256, attend_resident(sizeof(T), HD, QT)) void k_paged_attend(AttendArgs a) {
@@ -317,42 +319,38 @@ __global__ __launch_bounds__(256, attend_resident(sizeof(T), HD, QT)) void k_pag
   }
 
   const size_t head_at = (size_t)hk * a.p.head_units << 4;  // bytes
-  // Pages of 16 of the wave's steps at a time: lane 4j + i holds that of the i-th eight positions of step j.
+  // Pages are looked up two steps ahead, of positions behind the end the last one's.  They are checked where they are used: a check here would wait
+  // for the load, and with it for every load before it.
   const int ks0 = k_begin + 32 * wv;
-  auto pages_at = [&](int ks) {
-    const int pos = ks + 128 * (lane >> 2) + 8 * (lane & 3);
-    return pos < k_end ? paged_page(a.p, w.b, pos) : -1;
-  };
-  int pages = -1, pages_next = -1, pk = -1, pv = -1, pv_next = -1;
+  const int32_t *table = a.p.pages + w.b * a.p.pages_stride;
+  auto page_at = [&](int pos) { return table[(unsigned)min(pos, k_end - 1) >> a.p.page_shift]; };
+  auto is_there = [&](int page) { return (unsigned)page < (unsigned)a.p.n_pages; };
   St f;
+  int pv = -1, pk_next = -1, pv_next = -1;
   if (ks0 < k_end) {
-    pages = pages_at(ks0);
-    pages_next = pages_at(ks0 + 16 * 128);
-    pk = __shfl(pages, r >> 2, 64);
-    pv = __shfl(pages, g, 64);
-    load_keys<T, HD>(f, a.p, head_at, pk, ks0, r, g);
-    load_values<T, HD>(f, a.p, head_at, pv, ks0, r, g);
+    const int pk = page_at(ks0 + 8 * (r >> 2));
+    pv = page_at(ks0 + 8 * g);
+    load_keys<T, HD>(f, a.p, head_at, is_there(pk) ? pk : 0, ks0, r, g);
+    load_values<T, HD>(f, a.p, head_at, is_there(pv) ? pv : 0, ks0, r, g);
+    pk_next = page_at(ks0 + 128 + 8 * (r >> 2));
+    pv_next = page_at(ks0 + 128 + 8 * g);
   }
-  int j = 0;
-  bool odd = false;
-  for (int ks = ks0; ks < k_end; ks += 128) {
-    const bool more = ks + 128 < k_end;
-    if (more) {
-      if (++j == 16) {
-        j = 0;
-        pages = pages_next;
-        pages_next = pages_at(ks + 128 + 16 * 128);
-      }
-      pk = __shfl(pages, 4 * j + (r >> 2), 64);
-      pv_next = __shfl(pages, 4 * j + g, 64);
+  uint32_t odd = 0;
+  // (the last step is a copy without loads: loads behind a branch would make the waits in front of the products wait for all of them)
+  auto step = [&](int ks, auto more_) {
+    constexpr bool more = decltype(more_)::value;
+    const int pk = pk_next, pv_then = pv_next;
+    if constexpr (more) {
+      pk_next = page_at(ks + 256 + 8 * (r >> 2));
+      pv_next = page_at(ks + 256 + 8 * g);
     }
     float p[QT][8];
 #pragma unroll
     for (int t = 0; t < QT; ++t) scores<T, HD>(f, q[t], p[t]);
     // the keys are used: the next step's take their registers while the weights are worked out, and the next values' these values'
-    if (more) load_keys<T, HD>(f, a.p, head_at, pk, ks + 128, r, g);
+    if constexpr (more) load_keys<T, HD>(f, a.p, head_at, is_there(pk) ? pk : 0, ks + 128, r, g);
     // keys of this lane's scores: ks + 8g + i, in page pv
-    const bool whole = ks >= see_lo && ks + 32 <= min(see_hi, k_end) && __all(pv >= 0);
+    const bool there = is_there(pv), whole = ks >= see_lo && ks + 32 <= min(see_hi, k_end) && __all(there);
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       float(&sv)[8] = p[t];
@@ -361,7 +359,7 @@ __global__ __launch_bounds__(256, attend_resident(sizeof(T), HD, QT)) void k_pag
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int key = ks + 8 * g + i;
-          sv[i] = pv >= 0 && key <= pos[t] && key >= from && key < k_end ? sv[i] : -INFINITY;
+          sv[i] = there && key <= pos[t] && key >= from && key < k_end ? sv[i] : -INFINITY;
         }
       }
       const float top = max_of_quarters(fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])), fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7]))));
@@ -383,7 +381,7 @@ __global__ __launch_bounds__(256, attend_resident(sizeof(T), HD, QT)) void k_pag
     if (!whole) {  // positions that no row of the tile sees: their values, whatever they are, become zeros
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const bool live = pv >= 0 && ks + 8 * g + i < k_end;
+        const bool live = there && ks + 8 * g + i < k_end;
 #pragma unroll
         for (int x = 0; x < St::VW; ++x) f.v[i][x] = live ? f.v[i][x] : 0u;
       }
@@ -417,11 +415,16 @@ __global__ __launch_bounds__(256, attend_resident(sizeof(T), HD, QT)) void k_pag
             acc[t][ht] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(f.v[i][ht]), p[t][i], acc[t][ht], 0, 0, 0);
       }
     }
-    if (more) load_values<T, HD>(f, a.p, head_at, pv_next, ks + 128, r, g);
-    pv = pv_next;
+    if constexpr (more) load_values<T, HD>(f, a.p, head_at, is_there(pv_then) ? pv_then : 0, ks + 128, r, g);
+    pv = pv_then;
+  };
+  if (ks0 < k_end) {
+    int ks = ks0;
+    for (; ks + 128 < k_end; ks += 128) step(ks, std::true_type());
+    step(ks, std::false_type());
   }
 
-  if (__any(odd)) {  // this wave's steps of the positions outside [see_lo, see_hi) again
+  if (__any(odd != 0)) {  // this wave's steps of the positions outside [see_lo, see_hi) again
     for (int ks = ks0; ks < k_end; ks += 128) {
       if (ks >= see_lo && ks + 32 <= min(see_hi, k_end)) continue;
       for (int key = ks; key < min(ks + 32, k_end); ++key) {
@@ -429,12 +432,17 @@ __global__ __launch_bounds__(256, attend_resident(sizeof(T), HD, QT)) void k_pag
         if (page < 0) continue;
         const T *src = (const T *)(a.p.v + head_at + paged_row(a.p, page, key)) + 4 * VE * g;
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-          if (key > pos[t] || (a.window && key <= pos[t] - a.window)) continue;
+        for (int e = 0; e < 4; ++e) {
+          float v[VE];
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
+          for (int ht = 0; ht < HT; ++ht) v[ht] = only_odd<T>(src[VE * e + ht]);
 #pragma unroll
-            for (int ht = 0; ht < HT; ++ht) acc[t][ht][e] += only_odd<T>(src[VE * e + ht]);
+          for (int t = 0; t < QT; ++t) {
+            const bool sees = key <= pos[t] && !(a.window && key <= pos[t] - a.window);
+#pragma unroll
+            for (int ht = 0; ht < HT; ++ht) acc[t][ht][e] += sees ? v[ht] : 0.f;
+          }
+          __builtin_amdgcn_sched_barrier(0);  // (or all their conditions are held at once)
         }
       }
     }
@@ -516,6 +524,7 @@ __device__ __forceinline__ float max16(const f32x16_v &x) {
 // that reading one unit of 32 rows meets every bank; of values a thread loads 8 positions of 4 elements and turns them round on
 // the way to LDS.  The maximum follows the scores only when they have grown
 // by 2^8: weights up to 2^8 are as exact in 16 bits as weights up to 1, the sums are fp32, and most tiles then rescale nothing.
+constexpr int VALU = 0x2, MATRIX = 0x8, DS_READ = 0x100;  // kinds of instructions that sched_group_barrier tells apart
 constexpr int pc_lds(int NW) { return 4 * NW * 256 * 16; }
 
 template <class T, int HD, int NW>
@@ -552,10 +561,11 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
   const unsigned char *k_base = a.p.k + head_at, *v_base = a.p.v + head_at + 8 * vc;
   const int32_t *table = a.p.pages + w.b * a.p.pages_stride;
   const size_t pos_bytes = (size_t)a.p.pos_units << 4;
-  auto page_at = [&](int pos) {  // of a position before k_end; behind it, the last one's
-    const int page = table[(unsigned)min(pos, k_end - 1) >> a.p.page_shift];
-    return (unsigned)page < (unsigned)a.p.n_pages ? page : -1;
-  };
+  // Pages are looked up a tile ahead, of positions behind the end the last one's.  They are checked where they are used: a check here would wait
+  // for the load, and with it for every load before it.
+  auto page_at = [&](int pos) { return table[(unsigned)min(pos, k_end - 1) >> a.p.page_shift]; };
+  auto is_there = [&](int page) { return (unsigned)page < (unsigned)a.p.n_pages; };
+  auto row_at = [&](int page, int pos) { return paged_row(a.p, is_there(page) ? page : 0, pos); };
   // Row 32 u + 16 x + 8 y + 4 z + e of a key tile holds key 32 u + 16 x + 8 z + 4 y + e.  Wave instruction `it` fills 64 / NC rows; its
   // lanes' keys lie in one of two groups of eight positions, kgrp[it's].
   const int kgrp0 = NC == 16 ? 2 * wv : 4 * wv + (lane >> 5), kgrp1 = kgrp0 + (NC == 16 ? 1 : 2);
@@ -569,10 +579,10 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
     for (int it = 0; it < 4; ++it) {
       const int key = krow + (NC == 16 ? 8 * (it & 1) + 4 * (it >> 1) : 16 * (it >> 1) + 4 * (it & 1));
       const int unit = NC == 16 ? (lane ^ (lane >> 4)) % 16 ^ 4 * it : (lane ^ (lane >> 3)) % 8;  // by the row's number
-      const unsigned char *src = k_base + paged_row(a.p, max(pg.k[NC == 16 ? it & 1 : it >> 1], 0), ks + key) + 16 * unit;
+      const unsigned char *src = k_base + row_at(pg.k[NC == 16 ? it & 1 : it >> 1], ks + key) + 16 * unit;
       lanes_to_lds(src, (unsigned)((kbuf * UNITS + (wv * 4 + it) * 64) * 16));
     }
-    const unsigned char *src = v_base + paged_row(a.p, max(pg.v, 0), ks + 8 * kg);
+    const unsigned char *src = v_base + row_at(pg.v, ks + 8 * kg);
     x_page = pg.v;
 #pragma unroll
     for (int i = 0; i < 8; ++i) __builtin_memcpy(x[i], __builtin_assume_aligned(src + i * pos_bytes, 8), 8);
@@ -580,9 +590,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
   // Positions that some of the tile's rows see and others do not (those outside [all_lo, all_hi)): a weight of zero does not keep an infinity
   // or a NaN out of a product, so such values leave here and are added at the end for the rows that see them.
   const int all_hi = p0 + w.tile * R / a.G + 1, all_lo = a.window ? p0 + min(w.tile * R + R - 1, rows - 1) / a.G - a.window + 1 : 0;
-  bool odd = false;
+  uint32_t odd = 0;
   auto store = [&](int ks, int vbuf) {
-    const int live = x_page < 0 ? 0 : k_end - (ks + 8 * kg);  // positions behind the end hold anything
+    const int live = is_there(x_page) ? k_end - (ks + 8 * kg) : 0;  // positions behind the end hold anything
     if (live < 8) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) { x[i][0] = i < live ? x[i][0] : 0u; x[i][1] = i < live ? x[i][1] : 0u; }
@@ -602,7 +612,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
   };
   // loads to LDS have landed, reads of LDS are done; behind the barrier everyone's
   auto meet = [&]() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0), known to the compiler
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
@@ -625,6 +636,14 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) sc[u] = mat32<T>(kb[(32 * u + col) * NC + ((2 * kk + h) ^ (col & (NC - 1)))], q[kk], sc[u]);
     }
+    // four reads ahead of the products (left to itself the compiler has one or two: 443 -> 432 us for chunks of up to 2048 rows)
+    __builtin_amdgcn_sched_group_barrier(DS_READ, 4, 0);
+#pragma unroll
+    for (int i = 0; i < 2 * KK - 4; ++i) {
+      __builtin_amdgcn_sched_group_barrier(MATRIX, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(DS_READ, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(MATRIX, 4, 0);
   };
   // the maximum follows where it has to; -> what is taken off the scaled scores
   auto follow = [&]() {
@@ -652,7 +671,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
     return p;
   };
   // Tile t lies in buffers t % 2.  Lane i of a wave also looks whether the i-th eight positions of a tile are there at all.
-  auto there_at = [&](int ks) { return lane < KT / 8 ? page_at(ks + 8 * lane) : -1; };
+  auto there_at = [&](int ks) { return page_at(ks + 8 * (lane % (KT / 8))); };
   unsigned present = 0;
   Pages pages{{-1, -1}, -1};
   if (k_begin < k_end) {
@@ -660,7 +679,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
     fetch(k_begin, pages_of(k_begin), 0);
     pages = pages_of(k_begin + KT);
     store(k_begin, 0);
-    present = (unsigned)__ballot(there >= 0);
+    present = (unsigned)__ballot(is_there(there));
   }
   meet();
   int buf = 0;
@@ -695,9 +714,19 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
 #pragma unroll
         for (int j = 0; j < DT; ++j) acc[j] = mat32<T>(vs[(y * DT + j) * 64], p, acc[j]);
       }
+      // the later keys' weights between the earlier keys' products
+      __builtin_amdgcn_sched_group_barrier(DS_READ, 4, 0);
+      __builtin_amdgcn_sched_group_barrier(VALU, 30, 0);
+#pragma unroll
+      for (int i = 0; i < 4 * DT - 4; ++i) {
+        __builtin_amdgcn_sched_group_barrier(MATRIX, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(DS_READ, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(VALU, 28 / DT, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(MATRIX, 4, 0);
     }
     store(ks0 + KT, buf ^ 1);
-    present = (unsigned)__ballot(there >= 0);
+    present = (unsigned)__ballot(is_there(there));
     meet();
   }
 
@@ -714,7 +743,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
     for (int key = k_begin; key < k_end; ++key) {
       if (key >= all_lo && key < all_hi) { key = all_hi - 1; continue; }
       const int page = page_at(key);
-      if (page < 0 || key > pos || key < from) continue;
+      if (!is_there(page) || key > pos || key < from) continue;
       const T *src = (const T *)(a.p.v + head_at + paged_row(a.p, page, key));
 #pragma unroll
       for (int j = 0; j < DT; ++j)
@@ -809,11 +838,12 @@ __global__ __launch_bounds__(256) void k_paged_join(AttendArgs a, int align) {
 struct Shape {
   int qt, R, align, slots;             // slots: workgroups per key head that fill the chip
   int64_t tiles, units, cut, parts;    // per key head, at most: tiles, chunks, tiles that are cut, their chunks
+  bool whole;                          // no tile is cut
 };
 
 // Query rows of a tile: as few as hold a sequence's, since a tile reads the cache once for all of its rows.  Beyond 64 rows 128, or 256
 // where there are enough tiles of those.
-static Shape attend_shape(const spec_paged_cache *c, const spec_paged_batch *b, int n_q) {
+static Shape attend_shape(const spec_paged_cache *c, const spec_paged_batch *b, int n_q, int window) {
   Shape s{};
   const int64_t Hk = c->n_kv_heads, G = n_q / Hk, per = (int64_t)b->max_rows * G;
   auto tiles = [&](int R) { return std::min((int64_t)b->B * ((per + R - 1) / R), (int64_t)b->rows * G / R + b->B); };
@@ -823,16 +853,19 @@ static Shape attend_shape(const spec_paged_cache *c, const spec_paged_batch *b, 
   s.align = s.qt < 8 ? 128 : s.R * 64 / c->head_dim;
   s.tiles = tiles(s.R);
   s.slots = std::max(1, 256 * attend_resident((int)dtype_bytes(c->dtype), c->head_dim, s.qt) / (int)Hk);
-  const bool one = b->max_len <= PA_CHUNK_MIN;  // one chunk holds everything
-  s.units = s.tiles + (one ? 0 : s.slots);
-  s.cut = one ? 0 : std::min<int64_t>(s.tiles, s.slots * 2 / 3 + 1);
-  s.parts = one ? 0 : s.slots * 4 / 3 + 2;
+  // What a tile can need at most decides whether any is cut, and so whether there is a second kernel, which costs 5 us and more even where it finds
+  // nothing to join: the steps of 1536 positions that four waves share cost less, and a chunk's longer ones where there are enough tiles.
+  const int64_t span = window ? std::min<int64_t>(b->max_len, (int64_t)window + (s.R - 1) / G + 32) : b->max_len;
+  s.whole = span <= (s.qt < 8 ? 1536 : s.tiles * Hk >= 256 ? 2048 : 512);
+  s.units = s.tiles + (s.whole ? 0 : s.slots);
+  s.cut = s.whole ? 0 : std::min<int64_t>(s.tiles, s.slots * 2 / 3 + 1);
+  s.parts = s.whole ? 0 : s.slots * 4 / 3 + 2;
   return s;
 }
 static size_t attend_bytes(const spec_paged_cache *c, const Shape &s) {
   return (size_t)s.parts * c->n_kv_heads * s.R * (c->head_dim + 2) * sizeof(float);
 }
-static int attend_check(const char *who, const spec_paged_cache *c, const spec_paged_batch *b, int n_q, AttendArgs &a, Shape &s) {
+static int attend_check(const char *who, const spec_paged_cache *c, const spec_paged_batch *b, int n_q, int window, AttendArgs &a, Shape &s) {
   int rc = paged_args(who, c, b, &a.p);
   if (rc) return rc;
   if (n_q < 1 || n_q % c->n_kv_heads)
@@ -840,7 +873,7 @@ static int attend_check(const char *who, const spec_paged_cache *c, const spec_p
   a.G = n_q / c->n_kv_heads;
   if ((int64_t)b->rows * a.G >= 1 << 30) return fail_noctx(SPEC_ERR_CAPACITY, "%s: more than 2^30 query rows of a key head", who);
   if (b->B == 0 || b->rows == 0) { s = Shape{};  return SPEC_OK; }
-  s = attend_shape(c, b, n_q);
+  s = attend_shape(c, b, n_q, window);
   if (s.units * c->n_kv_heads * 512 >= (int64_t)1 << 32)
     return fail_noctx(SPEC_ERR_CAPACITY, "%s: %lld tiles of %d key heads are beyond one launch", who, (long long)s.units, c->n_kv_heads);
   return SPEC_OK;
@@ -883,7 +916,7 @@ extern "C" int spec_paged_attention_workspace_bytes(const spec_paged_cache *cach
   AttendArgs a{};
   Shape s;
   if (!bytes) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: bytes is null", who);
-  const int rc = attend_check(who, cache, batch, n_q_heads, a, s);
+  const int rc = attend_check(who, cache, batch, n_q_heads, 0, a, s);  // without a window: the largest need
   if (rc) return rc;
   *bytes = attend_bytes(cache, s);
   return SPEC_OK;
@@ -895,7 +928,7 @@ extern "C" int spec_paged_attention(void *hip_stream, const spec_paged_cache *ca
   const char *who = "spec_paged_attention";
   AttendArgs a{};
   Shape s;
-  int rc = attend_check(who, cache, batch, n_q_heads, a, s);
+  int rc = attend_check(who, cache, batch, n_q_heads, std::max(window, 0), a, s);
   if (rc) return rc;
   if (!(scale > 0.f) || std::isinf(scale)) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: scale must be positive and finite", who);
   if (window < 0) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: window=%d", who, window);
@@ -913,7 +946,7 @@ extern "C" int spec_paged_attention(void *hip_stream, const spec_paged_cache *ca
   a.sl2 = scale * 1.4426950408889634f;
   a.part = (float *)d_workspace;
   a.ml = need ? a.part + (size_t)s.parts * cache->n_kv_heads * s.R * cache->head_dim : nullptr;
-  a.chunk_min = PA_CHUNK_MIN;
+  a.chunk_min = s.whole ? 1 << 30 : PA_CHUNK_MIN;
   a.one_slot = 1.f / s.slots;
   hipStream_t st = (hipStream_t)hip_stream;
   if (s.qt == 16) {
