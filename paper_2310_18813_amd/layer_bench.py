@@ -8,6 +8,9 @@ The layer stack holds `--layers` distinct weight copies (default 4 = 1.6 GB, far
 
     python -m paper_2310_18813_amd.layer_bench --cells "1,0;8,3;64,3" --iters 20
 
+With --page every cell also times the cache append (with the rotary embedding) and the attention of one layer over a paged cache, the calls of a program
+that runs its products itself, and --kv-heads groups the query heads over fewer key heads there.
+
 Few kernel launches per run: this is also the program the rocprofv3 counter passes use.
 """
 import argparse
@@ -22,6 +25,34 @@ if ROOT not in sys.path:
 HBM_PEAK, MFMA_PEAK = 8.0e12, 2.5e15
 
 
+def paged_layer(B, torch, desc, dtype, nB, s, kv, page, kv_heads, iters):
+    """us of spec_paged_append and of spec_paged_attention for nB sequences of kv cached positions and s + 1 new rows each."""
+    H, td = desc["n_heads"], B.TORCH_DTYPE[B.DTYPE_CODE[dtype]]
+    hd, T, n = desc["d_model"] // H, nB * (s + 1), (kv + s + page) // page
+    pool = lambda: torch.randn((nB * n, page, kv_heads, hd), device="cuda:0").to(td)
+    cache = B.PagedCache(pool(), pool())
+    batch = B.PagedBatch(torch.randperm(nB * n, device="cuda:0").view(nB, n).to(torch.int32),
+                         torch.full((nB,), kv + s + 1, dtype=torch.int32, device="cuda:0"), T, max_len=kv + s + 1)
+    qkv = torch.randn((T, H + 2 * kv_heads, hd), device="cuda:0").to(td)
+    q, k, v = qkv.split([H, kv_heads, kv_heads], dim=1)
+    freq = B.spec_rope_frequencies(desc["rope_theta"], hd) if desc["pos_kind"] == 0 else None
+    x, out = torch.empty((T, H, hd), dtype=td, device="cuda:0"), torch.empty((T, H, hd), dtype=td, device="cuda:0")
+    space = torch.empty(B.spec_paged_attention_workspace_bytes(cache, batch, H), dtype=torch.uint8, device="cuda:0")
+    us = []
+    for call in (lambda: B.spec_paged_append(cache, batch, q, k, v, freq, out=x),
+                 lambda: B.spec_paged_attention(cache, batch, x, out=out, workspace=space)):
+        for _ in range(3):
+            call()
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        for _ in range(iters):
+            call()
+        e1.record()
+        e1.synchronize()
+        us.append(e0.elapsed_time(e1) * 1000.0 / iters)
+    return us
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--cells", default="1,0;1,8;8,3;16,3;64,0;64,3;64,8")
@@ -32,6 +63,8 @@ def main():
     ap.add_argument("--tune", default="0,0,0", help="spec_set_gemm_tuning arguments: tile_mtw,tile_nbw,flags")
     ap.add_argument("--attn-shape", type=int, default=0)
     ap.add_argument("--samples", type=int, default=0, help="also time this many single passes, one by one: median, p10, p90")
+    ap.add_argument("--page", type=int, default=0, help="also time append and attention over a cache in pages of this many positions")
+    ap.add_argument("--kv-heads", type=int, default=0, help="key heads of that cache (default: the model's heads)")
     args = ap.parse_args()
 
     import numpy as np
@@ -103,6 +136,12 @@ def main():
                     "kernels_us": {k: round(v[1] * 1000 / v[0], 1) for k, v in kt.items() if v[0]}})
         if spread:
             out[-1]["pass_spread"] = spread
+        if args.page:
+            kv_heads = args.kv_heads or desc["n_heads"]
+            append, attend = paged_layer(B, torch, desc, dtype, nB, s, args.kv, args.page, kv_heads, args.iters)
+            cached = 2 * 2 * nB * (args.kv + s + 1) * kv_heads * (d // desc["n_heads"])
+            out[-1]["paged"] = {"page": args.page, "kv_heads": kv_heads, "append_us": round(append, 1), "attention_us": round(attend, 1),
+                                "attention_hbm_frac": round(cached / HBM_PEAK / (attend * 1e-6), 3)}
         print(json.dumps(out[-1]), flush=True)
 
 
