@@ -42,24 +42,24 @@ __device__ __forceinline__ void load4(const T *row, int x, int V, float (&z)[4])
   }
 }
 
-template <class T, bool VEC>
-__global__ __launch_bounds__(256) void k_process_logits(LogitArgs a) {
+template <class T, bool VEC, int NT>
+__global__ __launch_bounds__(NT) void k_process_logits(LogitArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint32_t lr_smem[];
   uint32_t *cnt = lr_smem, *last = lr_smem + a.piece;  // counts; 1 + index of a token's bias (only with biases)
   const int b = blockIdx.y, c0 = blockIdx.x * a.piece, j0 = blockIdx.z * a.rows, j1 = min(j0 + a.rows, a.s + 1);
   const int words = a.r.n_bias ? 2 * a.piece : a.piece;
-  for (int x = 4 * threadIdx.x; x < words; x += 1024) *(uint4 *)(lr_smem + x) = make_uint4(0, 0, 0, 0);
+  for (int x = 4 * threadIdx.x; x < words; x += 4 * NT) *(uint4 *)(lr_smem + x) = make_uint4(0, 0, 0, 0);
   __syncthreads();
   if (a.r.d_tokens) {
     const int n = (int)min((int64_t)max(a.r.d_len[b], 0), a.r.tokens_stride), prompt = a.r.d_prompt_len ? a.r.d_prompt_len[b] : 0;
     const int32_t *tok = a.r.d_tokens + b * a.r.tokens_stride;
-    for (int i0 = threadIdx.x; i0 < n; i0 += 2048) {
+    for (int i0 = threadIdx.x; i0 < n; i0 += 8 * NT) {
       int v[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = tok[min(i0 + 256 * k, n - 1)];
+      for (int k = 0; k < 8; ++k) v[k] = tok[min(i0 + NT * k, n - 1)];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        const int i = i0 + 256 * k, x = v[k] - c0;
+        const int i = i0 + NT * k, x = v[k] - c0;
         if (i < n && v[k] >= c0 && v[k] < a.V && x < a.piece) {
           if (i < prompt) atomicOr(&cnt[x], LR_PROMPT);
           else atomicAdd(&cnt[x], 1u);
@@ -73,7 +73,7 @@ __global__ __launch_bounds__(256) void k_process_logits(LogitArgs a) {
     if (v >= c0 && v < a.V && v - c0 < a.piece) atomicOr(&cnt[v - c0], LR_PROPOSED);
   }
   const float *bias = a.r.d_bias + (int64_t)b * a.r.n_bias;
-  for (int i = threadIdx.x; i < a.r.n_bias; i += 256) {
+  for (int i = threadIdx.x; i < a.r.n_bias; i += NT) {
     const int v = a.r.d_bias_ids[(int64_t)b * a.r.n_bias + i];
     if (v >= c0 && v < a.V && v - c0 < a.piece) atomicMax(&last[v - c0], (uint32_t)(i + 1));
   }
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(256) void k_process_logits(LogitArgs a) {
   const T *rows = (const T *)a.logits + (int64_t)b * (a.s + 1) * a.row_stride;
   float *out = a.out + (int64_t)b * (a.s + 1) * a.V;
   const int mask_words = (a.V + 31) / 32;
-  for (int x = 4 * threadIdx.x; x < a.piece && c0 + x < a.V; x += 1024) {
+  for (int x = 4 * threadIdx.x; x < a.piece && c0 + x < a.V; x += 4 * NT) {
     const uint4 w4 = *(const uint4 *)(cnt + x);
     const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
     const bool seen = (w4.x | w4.y | w4.z | w4.w) != 0;
@@ -156,16 +156,22 @@ void launch_process_logits(const void *logits, int dtype, int64_t row_stride, in
                            const int32_t *t, int t_stride, float *out, hipStream_t st) {
   LogitArgs a{logits, row_stride, s, V, 1024, s + 1, r, t, t_stride, out};
   if (!r.d_mask) a.r.mask_rows = 1;
-  const int longest = r.n_bias ? 4096 : 8192;
-  while (a.piece < longest && (int64_t)B * ((V + 2 * a.piece - 1) / (2 * a.piece)) >= 1024) a.piece *= 2;
+  // Every workgroup of a sequence goes through all its tokens.  Where these can be many, workgroups of 512 threads and pieces that leave 1024
+  // workgroups (24 sequences x 8 rows of 151936 logits, up to 16000 tokens: 52.8 us; 256 threads 61.0, pieces half as long 58.1); else 256
+  // threads and 2048 workgroups (64 x 4 rows of 50272, up to 1000 tokens: 19.9 us; 512 threads 26.6, 512 workgroups 25.2).
+  const bool many = r.d_tokens && r.tokens_stride > 4096;
+  const int longest = r.n_bias ? 4096 : 8192, enough = many ? 1024 : 2048;
+  while (a.piece < longest && (int64_t)B * ((V + 2 * a.piece - 1) / (2 * a.piece)) >= enough) a.piece *= 2;
   const int pieces = (V + a.piece - 1) / a.piece;
   while (a.rows > LR_ROWS && (int64_t)B * pieces * ((s + a.rows) / a.rows) < 512) a.rows = (a.rows + 1) / 2;
   const size_t lds = (size_t)a.piece * (r.n_bias ? 8 : 4);
   const dim3 grid(pieces, B, (s + a.rows) / a.rows);
   SPEC_DISPATCH_DTYPE(dtype, T, {
     const bool vec = V % 4 == 0 && row_stride % 4 == 0 && (uintptr_t)logits % (4 * sizeof(T)) == 0 && (uintptr_t)out % 16 == 0;
-    if (vec) hipLaunchKernelGGL((k_process_logits<T, true>), grid, dim3(256), lds, st, a);
-    else hipLaunchKernelGGL((k_process_logits<T, false>), grid, dim3(256), lds, st, a);
+    if (many)
+      hipLaunchKernelGGL((vec ? k_process_logits<T, true, 512> : k_process_logits<T, false, 512>), grid, dim3(512), lds, st, a);
+    else
+      hipLaunchKernelGGL((vec ? k_process_logits<T, true, 256> : k_process_logits<T, false, 256>), grid, dim3(256), lds, st, a);
   });
 }
 
@@ -191,7 +197,7 @@ extern "C" int spec_process_logits(void *hip_stream, const void *d_logits, int32
   if ((const void *)d_out == d_logits && (dtype != SPEC_DTYPE_F32 || row_stride != vocab))
     return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: in place only for fp32 rows without padding", who);
   // a grid holds less than 2^32 threads
-  const int64_t per = ((int64_t)vocab + 1023) / 1024 * 4 * 256;
+  const int64_t per = ((int64_t)vocab + 1023) / 1024 * 4 * 512;
   const int most = (int)std::max<int64_t>(1, (((int64_t)1 << 32) - 1) / per);
   for (int b0 = 0; b0 < B; b0 += most) {
     const int nb = std::min(most, B - b0);
