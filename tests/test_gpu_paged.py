@@ -102,6 +102,9 @@ SHAPES = [  # heads, key heads, head_dim, page, rows per sequence, lengths
     (2, 1, 128, 8, [1, 2], [1700, 3]),                 # several chunks of one sequence beside a short one
     (5, 5, 64, 128, [3] * 70, list(range(3, 73))),     # more sequences than a wave has lanes
     (24, 2, 128, 32, [40, 2, 1, 70], [1100, 600, 2, 70]),
+    (4, 1, 128, 16, [2] * 65, [5000] + [9] * 30 + [2600] + [2] * 33),      # cut tiles among more sequences than a wave has lanes
+    (8, 1, 64, 16, [100, 40], [2300, 2100]),                               # cut tiles of many rows
+    (12, 4, 128, 8, [300, 1, 200], [310, 4000, 200]),                      # 256 rows a tile needs more of them: see the next test
 ]
 
 
@@ -209,8 +212,9 @@ def test_bounds_cut_what_lies_beyond(dtype):
     check(out, want, bound, owned_rows(c), 7.0)
 
 
-def test_offsets_beyond_32_bits():
-    """Four pages whose rows lie 2^31 elements apart and more."""
+@pytest.mark.parametrize("rows", [2, 70])
+def test_offsets_beyond_32_bits(rows):
+    """Four pages whose rows lie 2^31 elements apart and more; of 70 rows the first 40 are dead."""
     from paper_2310_18813_amd import binding as B
     page_stride = (1 << 31) + 4096
     store = torch.empty(3 * page_stride + 8192, dtype=torch.bfloat16, device=DEV)
@@ -222,21 +226,58 @@ def test_offsets_beyond_32_bits():
     vd.copy_(v)
     table = torch.tensor([[3, 1, 2, 0]], dtype=torch.int32)
     cache = B.PagedCache(kd, vd)
-    batch = B.PagedBatch(table.to(DEV), torch.tensor([30], dtype=torch.int32, device=DEV), 2)
-    q, nk, nv = (torch.randn((2, h, 64), generator=g).to(torch.bfloat16) for h in (3, 1, 1))
-    seqs = ref.sequences(1, 2, None, [30])
-    out = B.spec_paged_append(cache, batch, q.to(DEV), nk.to(DEV), nv.to(DEV), None)
+    batch = B.PagedBatch(table.to(DEV), torch.tensor([30], dtype=torch.int32, device=DEV), rows)
+    q, nk, nv = (torch.randn((rows, h, 64), generator=g).to(torch.bfloat16) for h in (3, 1, 1))
+    seqs = ref.sequences(1, rows, None, [30])
+    out = torch.full_like(q, 7.0).to(DEV)
+    B.spec_paged_append(cache, batch, q.to(DEV), nk.to(DEV), nv.to(DEV), None, out=out)
     qo, ko, vo, _, _ = ref.append(k, v, table, seqs, q, nk, nv, None)
-    assert torch.equal(kd.cpu().double(), ko) and torch.equal(vd.cpu().double(), vo) and torch.equal(out.cpu().double(), qo)
+    dead = max(0, rows - 30)
+    assert torch.equal(kd.cpu().double(), ko) and torch.equal(vd.cpu().double(), vo)
+    assert torch.equal(out.cpu().double()[dead:], qo[dead:]) and bool((out[:dead] == 7.0).all())
     got = B.spec_paged_attention(cache, batch, q.to(DEV))
     want, bound = ref.attention(ko.to(torch.bfloat16), vo.to(torch.bfloat16), table, seqs, q, 0.125, 0)
+    assert bool(((got.cpu().double() - want).abs() <= bound).all()) and not bool(got[:dead].any())
+
+
+@pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("fp16", 64)])
+@pytest.mark.parametrize("window", [0, 100])
+def test_tiles_of_256_rows(dtype, hd, window):
+    """Enough query rows for the largest tile; rows of every tile's start, middle and end are compared."""
+    from paper_2310_18813_amd import binding as B
+    c = Case(dtype, 64, 16, hd, 32, [900, 1, 1300], [1000, 700, 1500], seed=12)
+    q = c.rows_of(64)
+    cache, batch = c.on_gpu(B)
+    out = torch.full(q.shape, 7.0, dtype=c.td, device=DEV)
+    B.spec_paged_attention(cache, batch, q.to(DEV), window=window, out=out)
+    got = out.cpu().double()
+    assert bool((got[2201:] == 7.0).all()) and bool(torch.isfinite(got[:2201]).all())
+    for b, r0, n, kv in c.batch:
+        for i in sorted({0, 1, 63, 64, 127, n // 2, n - 65, n - 1} & set(range(n))):
+            p = kv - n + i
+            want, bound = ref.attention(c.k, c.v, c.table, [(b, 0, 1, p + 1)], q[r0 + i:r0 + i + 1], hd ** -0.5, window)
+            assert bool(((got[r0 + i] - want[0]).abs() <= bound[0]).all()), (b, i)
+
+
+def test_sequences_may_share_pages():
+    """A common prefix lies in the pool once; each sequence's own rows follow in pages of its own."""
+    from paper_2310_18813_amd import binding as B
+    c = Case("bf16", 8, 2, 64, 16, [2, 2, 2], [48, 40, 33], seed=13, extra_rows=0, ragged=False)
+    c.table[1, :2] = c.table[0, :2]
+    c.table[2, :2] = c.table[0, :2]
+    q = c.rows_of(8)
+    cache, batch = c.on_gpu(B)
+    got = B.spec_paged_attention(cache, batch, q.to(DEV))
+    want, bound = ref.attention(c.k, c.v, c.table, c.batch, q, 0.125, 0)
     assert bool(((got.cpu().double() - want).abs() <= bound).all())
 
 
-def test_captured_calls_follow_lengths_pages_and_rows_on_another_stream():
-    """Append and attention are captured once and replayed with other contents; eager calls on another stream lie between."""
+@pytest.mark.parametrize("rows,warm", [(3, True), (40, False)])
+def test_captured_calls_follow_lengths_pages_and_rows_on_another_stream(rows, warm):
+    """Append and attention are captured once and replayed with other contents; eager calls on another stream lie between.  Not
+    warm: the capture is the kernels' first use."""
     from paper_2310_18813_amd import binding as B
-    c = Case("bf16", 8, 2, 128, 16, [3, 3], [1500, 700], seed=8, ragged=False, extra_rows=0, fill=0.5)
+    c = Case("bf16", 8, 2, 128, 16, [rows, rows], [2500, 700], seed=8, ragged=False, extra_rows=0, fill=0.5)
     cache, batch = c.on_gpu(B)
     freq = B.spec_rope_frequencies(10000.0, 128)
     q, k, v = (c.rows_of(h).to(DEV) for h in (8, 2, 2))
@@ -251,11 +292,12 @@ def test_captured_calls_follow_lengths_pages_and_rows_on_another_stream():
 
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.stream(side):
-        both(out, space)
+        if warm:
+            both(out, space)
         side.synchronize()
         with torch.cuda.graph(graph, stream=side):
             both(out, space)
-    for lens in ([1500, 700], [3, 64], [900, 1490], [0, 2]):
+    for lens in ([2500, 700], [3, 64], [900, 690], [0, 2]):
         batch.lengths.copy_(torch.tensor(lens, dtype=torch.int32))
         q.normal_()
         k.normal_()
