@@ -628,14 +628,16 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
 
   // score e of sc[u]: key ks + 32 u + 16 (e / 8) + 8 h + e % 8
   f32x16_v sc[2];
+  // The two tiles' chains of products in turn: one that waits for the one before it takes twice the time of one that does not.
   auto key_products = [&](const u32x4_v *kb) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int e = 0; e < 16; ++e) sc[u][e] = 0.f;
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) sc[u] = mat32<T>(kb[(32 * u + col) * NC + ((2 * kk + h) ^ (col & (NC - 1)))], q[kk], sc[u]);
-    }
+    for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) sc[u] = mat32<T>(kb[(32 * u + col) * NC + ((2 * kk + h) ^ (col & (NC - 1)))], q[kk], sc[u]);
     // four reads ahead of the products (left to itself the compiler has one or two: 443 -> 432 us for chunks of up to 2048 rows)
     __builtin_amdgcn_sched_group_barrier(DS_READ, 4, 0);
 #pragma unroll
