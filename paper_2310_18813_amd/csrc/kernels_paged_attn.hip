@@ -507,15 +507,15 @@ template <class T> __device__ __forceinline__ f32x16_v mat32(u32x4_v a, u32x4_v 
 __device__ __forceinline__ void lanes_to_lds(const void *p, unsigned lds) {
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(lds), "v"(p) : "memory");
 }
-// The largest of 16.  Written as fmaxf, every score is first brought to canonical form by an instruction of its own.
-__device__ __forceinline__ float max16(const f32x16_v &x) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3\n\tv_max3_f32 %0, %0, %4, %5\n\tv_max3_f32 %0, %0, %6, %7\n\tv_max3_f32 %0, %0, %8, %9\n\t"
-      "v_max3_f32 %0, %0, %10, %11\n\tv_max3_f32 %0, %0, %12, %13\n\tv_max3_f32 %0, %0, %14, %15\n\tv_max_f32 %0, %0, %16"
-      : "=&v"(r)
+// The largest of top and x[0 .. 13].  Written as fmaxf, every score is first brought to canonical form by an instruction of its own.  The compiler
+// does not see what asm reads: top has to come from an instruction that reads the products' last result, so that it waits for them.
+__device__ __forceinline__ float max14(float top, const f32x16_v &x) {
+  asm("v_max3_f32 %0, %0, %1, %2\n\tv_max3_f32 %0, %0, %3, %4\n\tv_max3_f32 %0, %0, %5, %6\n\tv_max3_f32 %0, %0, %7, %8\n\t"
+      "v_max3_f32 %0, %0, %9, %10\n\tv_max3_f32 %0, %0, %11, %12\n\tv_max3_f32 %0, %0, %13, %14"
+      : "+v"(top)
       : "v"(x[0]), "v"(x[1]), "v"(x[2]), "v"(x[3]), "v"(x[4]), "v"(x[5]), "v"(x[6]), "v"(x[7]), "v"(x[8]), "v"(x[9]), "v"(x[10]), "v"(x[11]),
-        "v"(x[12]), "v"(x[13]), "v"(x[14]), "v"(x[15]));
-  return r;
+        "v"(x[12]), "v"(x[13]));
+  return top;
 }
 
 // A workgroup of NW waves takes 32 NW query rows, 32 a wave, and walks the positions in tiles of KT = 16 NW (heads of 128) or 32 NW (of 64):
@@ -649,7 +649,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
   };
   // the maximum follows where it has to; -> what is taken off the scaled scores
   auto follow = [&]() {
-    const float top = max_of_halves(fmaxf(max16(sc[0]), max16(sc[1])));
+    const float last2 = fmaxf(fmaxf(sc[0][14], sc[0][15]), fmaxf(sc[1][14], sc[1][15]));
+    const float top = max_of_halves(max14(max14(last2, sc[0]), sc[1]));
     if (__any(top > m + grow)) {
       const float mn = fmaxf(m, top), corr = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - mn) * a.sl2);
       m = mn;
@@ -709,6 +710,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
             sc[u][e] = key <= pos && key >= from && key < k_end && (here >> group & 1) ? sc[u][e] : -INFINITY;
           }
       }
+      __builtin_amdgcn_s_setprio(1);  // over the other wave's products, which run on by themselves (419 -> 413 us)
       const float off = follow();
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
@@ -726,6 +728,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
         __builtin_amdgcn_sched_group_barrier(VALU, 28 / DT, 0);
       }
       __builtin_amdgcn_sched_group_barrier(MATRIX, 4, 0);
+      __builtin_amdgcn_s_setprio(0);
     }
     store(ks0 + KT, buf ^ 1);
     present = (unsigned)__ballot(is_there(there));
