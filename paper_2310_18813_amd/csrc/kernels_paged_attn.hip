@@ -933,7 +933,10 @@ extern "C" int spec_paged_attention(void *hip_stream, const spec_paged_cache *ca
   const char *who = "spec_paged_attention";
   AttendArgs a{};
   Shape s;
-  int rc = attend_check(who, cache, batch, n_q_heads, std::max(window, 0), a, s);
+  // A window that reaches over all positions is none.  (So a window is at most 2^30, and its differences with positions stay inside 32 bits, those
+  // of dead rows as well.)
+  const bool endless = batch && window >= batch->max_len;
+  int rc = attend_check(who, cache, batch, n_q_heads, endless ? 0 : std::max(window, 0), a, s);
   if (rc) return rc;
   if (!(scale > 0.f) || std::isinf(scale)) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: scale must be positive and finite", who);
   if (window < 0) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: window=%d", who, window);
@@ -947,7 +950,7 @@ extern "C" int spec_paged_attention(void *hip_stream, const spec_paged_cache *ca
   a.out = (unsigned char *)d_out;
   a.q_stride = q_stride;
   a.out_stride = out_stride;
-  a.window = window;
+  a.window = endless ? 0 : window;
   a.sl2 = scale * 1.4426950408889634f;
   a.part = (float *)d_workspace;
   a.ml = need ? a.part + (size_t)s.parts * cache->n_kv_heads * s.R * cache->head_dim : nullptr;

@@ -122,6 +122,21 @@ def test_attention_matches_the_definition(dtype, shape, window):
     check(out, want, bound, owned_rows(c), 7.0)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("window", [99, 100, 101, 1 << 30, (1 << 31) - 1])
+@pytest.mark.parametrize("rows", [[9, 3, 20], [90, 70, 80]])
+def test_windows_as_long_as_the_longest_sequence_and_longer(dtype, window, rows):
+    """beside dead rows, whose positions are the lowest numbers that a window is taken from: the first tile begins with some"""
+    from paper_2310_18813_amd import binding as B
+    c = Case(dtype, 4, 2, 64, 16, rows, [4, 100, 2], seed=17)
+    q = c.rows_of(c.heads)
+    cache, batch = c.on_gpu(B, max_len=100)
+    out = torch.full(q.shape, 7.0, dtype=c.td, device=DEV)
+    B.spec_paged_attention(cache, batch, q.to(DEV), window=window, out=out)
+    want, bound = ref.attention(c.k, c.v, c.table, c.batch, q, 64 ** -0.5, window)
+    check(out, want, bound, owned_rows(c), 7.0)
+
+
 @pytest.mark.parametrize("layout", ["hnd", "pair"])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_attention_over_other_layouts_wide_rows_absent_pages_and_another_scale(layout, dtype):
