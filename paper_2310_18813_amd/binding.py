@@ -253,9 +253,11 @@ class LogitRules:
     def __init__(self, tokens=None, prompt_len=None, length=None, repetition=None, frequency=None, presence=None, bias_ids=None, bias=None, mask=None):
         every = (tokens, prompt_len, length, repetition, frequency, presence, bias_ids, bias, mask)
         self.tensors = every  # must outlive their use
-        self.B = None
+        self.B = self.on = None
         for t in every:
             if t is not None:
+                self.on = t.get_device() if self.on is None else self.on
+                assert t.get_device() == self.on >= 0  # all on one GPU
                 assert t.is_contiguous() or t is tokens and t.dim() == 2 and t.stride(1) == 1
                 self.B = t.shape[0] if self.B is None else self.B
                 assert t.shape[0] == self.B
@@ -279,15 +281,17 @@ def spec_process_logits(logits, rules, proposals=None, out=None):
     s0, s1, s2 = logits.stride()
     row = s1 if q > 1 else s0 if nB > 1 else V
     assert s2 == 1 and (nB < 2 or s0 == q * row)
+    on = logits.get_device()
+    assert on >= 0 and rules.on in (None, on)
     assert rules.B is None or rules.B == nB
     assert rules.mask_words is None or rules.mask_words == (V + 31) // 32
     pp = None
     if proposals is not None:
-        assert proposals.dtype is torch.int32 and proposals.shape == (nB, q - 1) and proposals.is_contiguous()
+        assert proposals.dtype is torch.int32 and proposals.shape == (nB, q - 1) and proposals.is_contiguous() and proposals.get_device() == on
         pp = proposals.data_ptr() or None
     if out is None:
         out = torch.empty(shape, dtype=torch.float32, device=logits.device)
-    assert out.dtype is torch.float32 and out.shape == shape and out.is_contiguous()
+    assert out.dtype is torch.float32 and out.shape == shape and out.is_contiguous() and out.get_device() == on
     _call(logits.device, lib.spec_process_logits, logits.data_ptr(), _DTYPE_OF[logits.dtype], row, nB, q - 1, V, rules.ref, pp, out.data_ptr())
     return out
 
@@ -320,7 +324,8 @@ class PagedBatch:
         assert lengths.dim() == 1 and lengths.dtype == torch.int32 and lengths.is_contiguous()
         assert row_start is None or (row_start.dtype == torch.int32 and row_start.shape == (nB + 1,) and row_start.is_contiguous())
         self.pages, self.lengths, self.row_start = pages, lengths, row_start  # must outlive their use
-        self.rows, self.max_len = rows, max_len
+        self.rows, self.max_len, self.on = rows, max_len, lengths.get_device()
+        assert pages.get_device() == self.on >= 0 and (row_start is None or row_start.get_device() == self.on)
         stride = pages.stride(0) if nB > 1 else pages.shape[1]
         if max_rows is None:
             max_rows = rows if row_start is not None else max(1, rows // max(1, nB))
@@ -329,6 +334,7 @@ class PagedBatch:
         self.ref, self._page_size = C.byref(self.desc), None
 
     def _for(self, cache):
+        assert cache.device.index == self.on
         if cache.page_size != self._page_size:
             most = self.pages.shape[1] * cache.page_size
             assert self.max_len is None or self.max_len <= most
@@ -392,6 +398,7 @@ def spec_paged_attention(cache, batch, q, scale=None, window=0, out=None, worksp
     assert no == nq
     if workspace is None:
         workspace = torch.empty(spec_paged_attention_workspace_bytes(cache, batch, nq), dtype=torch.uint8, device=q.device)
+    assert workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.get_device() == batch.on
     _call(cache.device, lib.spec_paged_attention, cache.ref, batch._for(cache), nq, qp, qs, cache.scale if scale is None else scale, window,
           workspace.data_ptr() or None, workspace.numel(), op, os_)
     return out
@@ -610,6 +617,7 @@ class Context:
             self._rules = None
             return None
         V = self.tgt_desc["vocab"]
+        assert rules.on in (None, self.workspace.get_device())
         assert rules.B in (None, self.B_max) and rules.mask_words in (None, (V + 31) // 32)
         tl = torch.zeros((self.B_max * (self.s_max + 1), V), dtype=torch.float32, device=self.device)
         _check(lib.spec_set_logit_rules(self.h, C.byref(rules.desc), _dp(tl)), self.h)

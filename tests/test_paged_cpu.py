@@ -2,6 +2,7 @@
 import ctypes as C
 
 import pytest
+import torch
 
 FAKE = 4096  # never dereferenced: validation fails first
 
@@ -98,3 +99,15 @@ def test_logit_rules_arguments(B):
         assert call(**kw) == B.ERR_CAPACITY, kw
     assert call(nB=0, logits=None, out=None) == B.OK
     assert B.lib.spec_set_logit_rules(None, None, None) == B.ERR_INVALID_ARG
+
+
+def test_tensors_of_the_host_are_refused(B):
+    """a kernel would take their addresses for the device's"""
+    i32 = dict(dtype=torch.int32)
+    with pytest.raises(AssertionError):
+        B.PagedBatch(torch.zeros((2, 4), **i32), torch.ones(2, **i32), 2)
+    for kw in (dict(length=torch.zeros(2, **i32)), dict(repetition=torch.ones(2)), dict(mask=torch.zeros((2, 1, 4), **i32))):
+        with pytest.raises(AssertionError):
+            B.LogitRules(**kw)
+    with pytest.raises(AssertionError):
+        B.spec_process_logits(torch.zeros((2, 1, 64)), B.LogitRules())
