@@ -367,7 +367,8 @@ typedef struct {
    (SPEC_DTYPE_*), row_stride elements apart (a head whose rows are padded); d_proposals [B][s] (NULL when s = 0, or when
    proposals do not count); d_out [B][s+1][vocab] fp32, what the acceptance rules take.  d_out may be d_logits itself
    where the type is fp32 and row_stride = vocab.  Enqueues one kernel on hip_stream (NULL = the default stream), needs no
-   context and no workspace, does not wait.  s <= 15, B <= 65535, vocab <= 2^28 (SPEC_ERR_CAPACITY).
+   context and no workspace, does not wait (more kernels than one beyond 2^32 threads).  s <= 15, B <= 65535, vocab <= 2^28,
+   tokens_stride < 2^30 (SPEC_ERR_CAPACITY).
 
    spec_set_logit_rules: the same rules inside a context, for every following round: they apply to the target's logits
    before the greedy tokens are taken, or before spec_set_sampling's rule.  The tokens are the context's own (d_tokens,
@@ -400,7 +401,10 @@ int spec_set_logit_rules(spec_ctx *ctx, const spec_logit_rules *rules, float *d_
    behind the last sequence belong to none.  Position p lies in page d_pages[b * pages_stride + p / page_size]; an entry
    outside [0, n_pages) is an absent page: nothing is written to it and no row sees its positions.  max_rows and max_len
    are the host's bounds of n_b and d_len[b]: grids and workspaces follow them, what lies beyond is not processed
-   (n_b counts as max_rows, d_len[b] as max_len). */
+   (n_b counts as max_rows, d_len[b] as max_len).
+
+   SPEC_ERR_CAPACITY: more than 65535 sequences, max_len beyond 2^30, a cache stride of 64 GB or more, 2^30 or more query rows of
+   a key head (rows * n_q_heads / n_kv_heads), or more work than one launch holds (2^32 threads). */
 typedef struct {
   int32_t dtype;                             /* SPEC_DTYPE_*: of the cache and of every row-wise tensor */
   int32_t head_dim, n_kv_heads, page_size, n_pages;
@@ -432,7 +436,7 @@ int spec_paged_append(void *hip_stream, const spec_paged_cache *cache, const spe
                       const double *d_inv_freq, int32_t rope_dim, void *d_q_out, int64_t q_out_stride);
 
 /* Attention of every row over its sequence's pages, causal: row at position p sees positions max(0, p - window + 1) .. p
-   (window = 0: from 0 on).  Query head h reads key head h / (n_q_heads / n_kv_heads).  out = sum of softmax(scale * q.k)
+   (window = 0, or max_len and more: from 0 on).  Query head h reads key head h / (n_q_heads / n_kv_heads).  out = sum of softmax(scale * q.k)
    times v; a row that sees nothing is zeros, and what lies at positions that a row does not see never reaches it, be it
    infinite or NaN.  Scores, softmax and sums are fp32; softmax weights of 16-bit runs are rounded to the type once for the product
    with the values.  n_q_heads a multiple of n_kv_heads; scale > 0.

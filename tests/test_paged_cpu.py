@@ -43,7 +43,8 @@ def test_cache_and_batch_descriptions(B):
                  (dict(page_size=4), B.ERR_UNSUPPORTED), (dict(page_size=2048), B.ERR_UNSUPPORTED), (dict(n_pages=0), B.ERR_INVALID_ARG),
                  (dict(n_kv_heads=0), B.ERR_INVALID_ARG), (dict(d_k=None), B.ERR_INVALID_ARG), (dict(d_v=FAKE + 8), B.ERR_INVALID_ARG),
                  (dict(pos_stride=252), B.ERR_INVALID_ARG), (dict(pos_stride=64), B.ERR_INVALID_ARG), (dict(head_stride=64), B.ERR_INVALID_ARG),
-                 (dict(page_stride=-4096), B.ERR_INVALID_ARG)]
+                 (dict(page_stride=-4096), B.ERR_INVALID_ARG), (dict(page_stride=1 << 35), B.ERR_CAPACITY), (dict(pos_stride=1 << 35), B.ERR_CAPACITY),
+                 (dict(head_stride=1 << 35), B.ERR_CAPACITY)]
     bad_batch = [(dict(B=-1), B.ERR_INVALID_ARG), (dict(rows=-1), B.ERR_INVALID_ARG), (dict(B=65536, rows=65536), B.ERR_CAPACITY),
                  (dict(rows=7), B.ERR_INVALID_ARG), (dict(max_rows=2), B.ERR_INVALID_ARG), (dict(max_rows=7), B.ERR_INVALID_ARG),
                  (dict(max_rows=0, d_row_start=FAKE), B.ERR_INVALID_ARG), (dict(max_len=161), B.ERR_INVALID_ARG), (dict(max_len=0), B.ERR_INVALID_ARG),
