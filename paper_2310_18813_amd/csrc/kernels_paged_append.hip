@@ -2,8 +2,8 @@
 // element i of a head turns with i + R/2 by the angle position * inv_freq[i]).
 //
 // One pass over q, k and v: 2 * rows * (Hq + 2 Hkv) * hd elements move, three operations a rotated element, so memory bounds it, and
-// with few rows the chain length -> page -> store does.  4548 rows of 52 + 104 heads of 128, fp16: 72 us a call for 363 MB (5.0 TB/s); 256 rows
-// of 32 + 16 heads, bf16: 3.9 us in the kernel.
+// with few rows the chain length -> page -> store does.  4548 rows of 52 + 104 heads of 128, fp16: 74 us a call for 363 MB (4.9 TB/s); 256 rows
+// of 32 + 16 heads, bf16: 3.7 us a call in a captured graph.
 #include "paged.h"
 
 namespace spec {

@@ -10,8 +10,8 @@
 // The first product's result layout (lane = query, 4 keys a lane and tile) is the second's operand layout once row 4g + i of key tile t
 // carries key 8g + 4t + i.  Keys come from memory in operand order; of values a lane loads the same 8 or 4 elements of 8
 // positions, whole rows of a head across 16 lanes, and turns the block round in registers.
-// Few rows are bound by their loads: 64 sequences x 4 rows of 32 heads of 128 over up to 1000 positions, bf16, 650 MB in 124 us
-// (5.2 TB/s), and the loads without any arithmetic took as long.  Six sequences of up to 32000 positions, 32 heads over 8: 101 us.
+// Few rows are bound by their loads: 64 sequences x 4 rows of 32 heads of 128 over up to 1000 positions, bf16, 650 MB in 125 us
+// (5.2 TB/s), and the loads without any arithmetic took as long.  Six sequences of up to 32000 positions, 32 heads over 8: 102 us.
 //
 // Chunks: a sequence with more rows or positions has more work, and the host does not know the lengths.  Every wave adds the
 // batch's work up (a load and a few ALU instructions) and cuts it by what an even share would be, whatever the lengths are.
@@ -526,7 +526,7 @@ __device__ __forceinline__ float max14(float top, const f32x16_v &x) {
 // that reading one unit of 32 rows meets every bank; of values a thread loads 8 positions of 4 elements and turns them round on
 // the way to LDS.  The maximum follows the scores only when they have grown
 // by 2^8: weights up to 2^8 are as exact in 16 bits as weights up to 1, the sums are fp32, and most tiles then rescale nothing.
-// Chunks of up to 2048 rows over 8192 positions, 32 heads over 8, bf16: 415 us (917 TFLOP/s), products busy 42 % of the clocks.
+// Chunks of up to 2048 rows over 8192 positions, 32 heads over 8, bf16: 417 us (913 TFLOP/s), products busy 42 % of the clocks.
 constexpr int VALU = 0x2, MATRIX = 0x8, DS_READ = 0x100;  // kinds of instructions that sched_group_barrier tells apart
 constexpr int pc_lds(int NW) { return 4 * NW * 256 * 16; }
 
