@@ -310,6 +310,8 @@ __global__ __launch_bounds__(256, attend_resident(sizeof(T), HD, QT)) void k_pag
   // every row of the tile sees all positions [see_lo, see_hi)
   const int i0 = w.tile * R / a.G, i1 = min(s.n - 1, (w.tile * R + R - 1) / a.G);
   const int see_hi = s.kv - s.n + i0 + 1, see_lo = a.window ? s.kv - s.n + i1 - a.window + 1 : 0;
+  // the first position that any of them sees (the first step, a multiple of 32, can begin before it)
+  const int any_lo = a.window ? s.kv - s.n + i0 - a.window + 1 : 0;
 
   float m[QT], l[QT];
   f32x4_v acc[QT][HT];
@@ -383,7 +385,8 @@ __global__ __launch_bounds__(256, attend_resident(sizeof(T), HD, QT)) void k_pag
     if (!whole) {  // positions that no row of the tile sees: their values, whatever they are, become zeros
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const bool live = there && ks + 8 * g + i < k_end;
+        const int key = ks + 8 * g + i;
+        const bool live = there && key >= any_lo && key < k_end;
 #pragma unroll
         for (int x = 0; x < St::VW; ++x) f.v[i][x] = live ? f.v[i][x] : 0u;
       }
