@@ -593,9 +593,11 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) __builtin_memcpy(x[i], __builtin_assume_aligned(src + i * pos_bytes, 8), 8);
   };
-  // Positions that some of the tile's rows see and others do not (those outside [all_lo, all_hi)): a weight of zero does not keep an infinity
-  // or a NaN out of a product, so such values leave here and are added at the end for the rows that see them.
+  // All rows of the workgroup see [all_lo, all_hi).  Beyond, where some do and others do not, a weight of zero does not keep an infinity or a NaN
+  // out of a product: from tiles of positions that reach beyond (odd_tile) all such values leave here, and are added at the end for
+  // the rows that see them.
   const int all_hi = p0 + w.tile * R / a.G + 1, all_lo = a.window ? p0 + min(w.tile * R + R - 1, rows - 1) / a.G - a.window + 1 : 0;
+  auto odd_tile = [&](int ks) { return ks + KT > all_hi || ks < all_lo; };
   uint32_t odd = 0;
   auto store = [&](int ks, int vbuf) {
     const int live = is_there(x_page) ? k_end - (ks + 8 * kg) : 0;  // positions behind the end hold anything
@@ -603,7 +605,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) { x[i][0] = i < live ? x[i][0] : 0u; x[i][1] = i < live ? x[i][1] : 0u; }
     }
-    if (ks + KT > all_hi || ks < all_lo) {
+    if (odd_tile(ks)) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) { odd |= drop_odd<T>(x[i][0]); odd |= drop_odd<T>(x[i][1]); }
     }
@@ -753,7 +755,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
   if (any) {
     const int from = a.window ? pos - a.window + 1 : 0;
     for (int key = k_begin; key < k_end; ++key) {
-      if (key >= all_lo && key < all_hi) { key = all_hi - 1; continue; }
+      if ((key - k_begin) % KT == 0 && !odd_tile(key)) { key += KT - 1; continue; }
       const int page = page_at(key);
       if (!is_there(page) || key > pos || key < from) continue;
       const T *src = (const T *)(a.p.v + head_at + paged_row(a.p, page, key));

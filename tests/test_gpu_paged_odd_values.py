@@ -43,3 +43,54 @@ def test_what_lies_in_front_of_the_window_never_reaches_a_tile_of_one_position(d
     want, bound = ref.attention(c.k, c.v, c.table, c.batch, q, hd ** -0.5, window)
     assert bool(torch.isfinite(want).all())
     check_odd(attend(c, q, window), want, bound)
+
+
+def plant(c, b, positions):
+    """one odd value at each position, in an element of its own -> [(position, element, value)]"""
+    planted = [(p, i % c.hd, ODD[i % 3]) for i, p in enumerate(positions)]
+    assert len(planted) <= c.hd
+    for p, d, x in planted:
+        page = int(c.table[b, p // c.page])
+        assert 0 <= page < c.n_pages
+        c.v[page, p % c.page, :, d] = x
+    return planted
+
+
+def borders(rows, kv, G, window):
+    """positions on both sides of what all rows of a tile see, for tiles of 16 to 256 query rows, and early ones"""
+    at, p0 = {0, 25, kv - 1}, kv - rows
+    for R in (16, 32, 64, 128, 256):
+        for t in range(3):
+            i0, i1 = t * R // G, min(rows - 1, (t * R + R - 1) // G)
+            at |= {p0 + i0, p0 + i0 + 1} | ({p0 + i1 - window + 1, p0 + i1 - window, p0 + i0 - window + 1} if window else set())
+    return sorted(p for p in at if 0 <= p < kv)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("shape", [(4, 2, 128, 150, 210), (4, 2, 64, 150, 210), (4, 2, 128, 150, 150), (2, 2, 128, 150, 1100), (8, 2, 64, 6, 300),
+                                   (16, 1, 128, 3, 3000)], ids=lambda s: "h%dk%dd%d_%drows_%d" % s)
+@pytest.mark.parametrize("window", [0, 40, 100])
+def test_what_a_row_sees_shows(dtype, shape, window):
+    """Also where other rows of the same tile do not see it."""
+    heads, kv_heads, hd, rows, kv = shape
+    c = Case(dtype, heads, kv_heads, hd, 16, [rows, 1], [kv, 50], seed=kv + window)
+    plant(c, 0, borders(rows, kv, heads // kv_heads, window)[:hd])
+    q = c.rows_of(heads)
+    want, bound = ref.attention(c.k, c.v, c.table, c.batch, q, hd ** -0.5, window)
+    got = attend(c, q, window)
+    assert not bool(torch.isfinite(want[:rows]).all())
+    check_odd(got[:rows + 1], want[:rows + 1], bound[:rows + 1])
+
+
+@pytest.mark.parametrize("dtype,hd", [("bf16", 128), ("fp16", 64)])
+@pytest.mark.parametrize("window", [0, 100])
+def test_what_a_row_sees_shows_in_tiles_of_256_rows(dtype, hd, window):
+    heads, kv_heads, rows, lens = 64, 16, [900, 1, 1300], [1000, 700, 1500]
+    c = Case(dtype, heads, kv_heads, hd, 32, rows, lens, seed=12)
+    seen = torch.zeros((c.T, hd), dtype=torch.bool)
+    for b, r0, n, kv in c.batch:
+        pos = torch.arange(kv - n, kv)
+        for p, d, x in plant(c, b, borders(n, kv, heads // kv_heads, window)[:hd]):
+            seen[r0:r0 + n, d] |= (pos >= p) & ((pos - p < window) if window else True)
+    got = attend(c, c.rows_of(heads), window)[:sum(rows)]
+    assert bool(seen.any()) and torch.equal(~torch.isfinite(got), seen[:sum(rows), None].expand_as(got))
