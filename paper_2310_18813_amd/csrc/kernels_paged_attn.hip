@@ -313,6 +313,8 @@ __global__ __launch_bounds__(256, attend_resident(sizeof(T), HD, QT)) void k_pag
   // the first position that any of them sees (the first step, a multiple of 32, can begin before it)
   const int any_lo = a.window ? s.kv - s.n + i0 - a.window + 1 : 0;
 
+  auto all_see = [&](int ks) { return ks >= see_lo && ks + 32 <= min(see_hi, k_end); };
+
   float m[QT], l[QT];
   f32x4_v acc[QT][HT];
 #pragma unroll
@@ -354,7 +356,7 @@ __global__ __launch_bounds__(256, attend_resident(sizeof(T), HD, QT)) void k_pag
     // the keys are used: the next step's take their registers while the weights are worked out, and the next values' these values'
     if constexpr (more) load_keys<T, HD>(f, a.p, head_at, is_there(pk) ? pk : 0, ks + 128, r, g);
     // keys of this lane's scores: ks + 8g + i, in page pv
-    const bool there = is_there(pv), whole = ks >= see_lo && ks + 32 <= min(see_hi, k_end) && __all(there);
+    const bool there = is_there(pv), alike = all_see(ks), whole = alike && __all(there);
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       float(&sv)[8] = p[t];
@@ -392,7 +394,7 @@ __global__ __launch_bounds__(256, attend_resident(sizeof(T), HD, QT)) void k_pag
       }
       // Positions that some of the tile's rows see and others do not: a weight of zero does not keep an infinity or a NaN out of a
       // product, so such values leave here and are added at the end for the rows that see them.
-      if (i0 != i1) {
+      if (i0 != i1 && !alike) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -429,9 +431,9 @@ __global__ __launch_bounds__(256, attend_resident(sizeof(T), HD, QT)) void k_pag
     step(ks, std::false_type());
   }
 
-  if (__any(odd != 0)) {  // this wave's steps of the positions outside [see_lo, see_hi) again
+  if (__any(odd != 0)) {  // this wave's steps that hold positions outside [see_lo, see_hi) again
     for (int ks = ks0; ks < k_end; ks += 128) {
-      if (ks >= see_lo && ks + 32 <= min(see_hi, k_end)) continue;
+      if (all_see(ks)) continue;
       for (int key = ks; key < min(ks + 32, k_end); ++key) {
         const int page = paged_page(a.p, w.b, key);
         if (page < 0) continue;

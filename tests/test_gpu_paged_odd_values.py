@@ -94,3 +94,16 @@ def test_what_a_row_sees_shows_in_tiles_of_256_rows(dtype, hd, window):
             seen[r0:r0 + n, d] |= (pos >= p) & ((pos - p < window) if window else True)
     got = attend(c, c.rows_of(heads), window)[:sum(rows)]
     assert bool(seen.any()) and torch.equal(~torch.isfinite(got), seen[:sum(rows), None].expand_as(got))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("rows", [6, 150])
+@pytest.mark.parametrize("page,absent,at", [(16, (0, 2, 9), (16, 20, 31, 50, 63, 135, 145)), (8, (1, 6, 7), (0, 3, 17, 40, 63))])
+def test_what_a_row_sees_shows_beside_an_absent_page(dtype, rows, page, absent, at):
+    """the odd values lie among the 32 positions that the absent page is one of"""
+    c = Case(dtype, 4, 2, 128, page, [rows], [rows + 180], seed=page, absent=[(0, j) for j in absent])
+    plant(c, 0, [p for p in at if p // page not in absent])
+    q = c.rows_of(4)
+    want, bound = ref.attention(c.k, c.v, c.table, c.batch, q, 128 ** -0.5, 0)
+    assert not bool(torch.isfinite(want[:rows]).all())
+    check_odd(attend(c, q)[:rows], want[:rows], bound[:rows])
