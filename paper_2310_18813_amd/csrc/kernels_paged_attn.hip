@@ -71,6 +71,10 @@ __device__ __forceinline__ float max_of_quarters(float v) {  // of lanes i, i ^ 
   return max_of_halves(fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1])));
 }
 
+// A row's maximum score and sum of weights if it sees nothing.  (A sum of zero alone can also mean that the scaled scores overflow, which gives NaN
+// as the softmax of infinite scores does.)
+__device__ __forceinline__ bool nothing_seen(float m, float l) { return m == -INFINITY && l == 0.f; }
+
 // A sequence's part of the work: its tiles of R query rows, the positions that one of them can need at most, its chunks.
 struct Share { int tiles, span, chunks, len; };
 __device__ __forceinline__ Share share_of(const AttendArgs &a, const PagedSeq &s, int R) {
@@ -493,11 +497,12 @@ __global__ __launch_bounds__(256, attend_resident(sizeof(T), HD, QT)) void k_pag
         for (int d = 0; d < VE; ++d) dst[d] = o[d];
         if (d0 == 0) { a.ml[(slot + 16 * t + row) * 2] = mr; a.ml[(slot + 16 * t + row) * 2 + 1] = lr; }
       } else {
-        const float inv = lr == 0.f ? 0.f : 1.f / lr;
+        const bool none = nothing_seen(mr, lr);
+        const float inv = 1.f / lr;
         const int i = f / a.G;
         T *dst = (T *)a.out + (s.row0 + i) * a.out_stride + (hk * a.G + f - i * a.G) * HD + d0;
 #pragma unroll
-        for (int d = 0; d < VE; ++d) Conv<T>::st(dst, d, lr == 0.f ? 0.f : o[d] * inv);
+        for (int d = 0; d < VE; ++d) Conv<T>::st(dst, d, none ? 0.f : o[d] * inv);
       }
     }
   }
@@ -774,7 +779,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
   // element 4 c + i of the query lies in tile i / IPT, row c + VC (i % IPT); a lane holds the rows 8 (e / 4) + 4 h + e % 4
   const bool several = w.chunks > 1;
   const int64_t at = ((int64_t)w.part * Hk + hk) * R + 32 * wv + col;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const bool none = nothing_seen(m, l);
+  const float inv = 1.f / l;
   T *dst = (T *)a.out + (s.row0 + qi) * a.out_stride + (hk * a.G + f - qi * a.G) * HD;
   if (several && h == 0) { a.ml[at * 2] = m; a.ml[at * 2 + 1] = l; }
 #pragma unroll
@@ -793,7 +799,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
       for (int y = 0; y < 2; ++y) {
         u32x4_v v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = Mat<T>::pack2(l == 0.f ? 0.f : o[8 * y + 2 * i] * inv, l == 0.f ? 0.f : o[8 * y + 2 * i + 1] * inv);
+        for (int i = 0; i < 4; ++i) v[i] = Mat<T>::pack2(none ? 0.f : o[8 * y + 2 * i] * inv, none ? 0.f : o[8 * y + 2 * i + 1] * inv);
         *(u32x4_v *)(dst + d + 8 * y) = v;
       }
     }
@@ -843,11 +849,12 @@ __global__ __launch_bounds__(256) void k_paged_join(AttendArgs a, int align) {
       for (int d = 0; d < VE; ++d) o[d] += y[i][d / 4][d % 4] * wt;
     }
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const bool none = nothing_seen(m, l);
+  const float inv = 1.f / l;
   const int i = f / a.G;
   T *dst = (T *)a.out + (s.row0 + i) * a.out_stride + (hk * a.G + f - i * a.G) * HD + d0;
 #pragma unroll
-  for (int d = 0; d < VE; ++d) Conv<T>::st(dst, d, l == 0.f ? 0.f : o[d] * inv);
+  for (int d = 0; d < VE; ++d) Conv<T>::st(dst, d, none ? 0.f : o[d] * inv);
 }
 
 // ------------------------------------------------------------------ launch
