@@ -634,7 +634,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
   };
 
   float m = -INFINITY, l = 0.f;
-  const float grow = 8.f / a.sl2;
+  const float grow = fminf(8.f / a.sl2, 3.4e38f);  // (finite: the maximum starts at -infinity)
   f32x16_v acc[DT];
 #pragma unroll
   for (int j = 0; j < DT; ++j)

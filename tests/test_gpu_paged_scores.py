@@ -1,7 +1,8 @@
-"""spec_paged_attention at the ends of the numbers' ranges: scores beyond fp32."""
+"""spec_paged_attention at the ends of the numbers' ranges: scores beyond fp32, the smallest scales."""
 import pytest
 import torch
 
+import paged_reference as ref
 from test_gpu_paged import Case
 
 pytestmark = pytest.mark.gpu
@@ -24,3 +25,14 @@ def test_scores_beyond_fp32_are_not_taken_for_nothing_seen(dtype, rows, lens):
     got = attend(c, torch.full((c.T, 4, 64), 1e5, dtype=c.td), scale=1e30)
     n = sum(rows)
     assert bool(torch.isnan(got[:n]).all()) and not bool(got[n:n + 2].any()) and bool(torch.isnan(got[n + 2]).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("rows,lens", ROWS)
+@pytest.mark.parametrize("scale", [1e-30, 1.2e-38, 1e-40])
+def test_the_smallest_scales_give_every_position_the_same_weight(dtype, rows, lens, scale):
+    c = Case(dtype, 4, 1, 64, 16, rows, lens, seed=2, extra_rows=0)
+    q = c.rows_of(4)
+    want, bound = ref.attention(c.k, c.v, c.table, c.batch, q, scale, 0)
+    got = attend(c, q, scale=scale)
+    assert bool(((got - want).abs() <= bound).all())
