@@ -956,7 +956,8 @@ extern "C" int spec_paged_attention(void *hip_stream, const spec_paged_cache *ca
   const bool endless = batch && window >= batch->max_len;
   int rc = attend_check(who, cache, batch, n_q_heads, endless ? 0 : std::max(window, 0), a, s);
   if (rc) return rc;
-  if (!(scale > 0.f) || std::isinf(scale)) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: scale must be positive and finite", who);
+  a.sl2 = scale * 1.4426950408889634f;
+  if (!(scale > 0.f) || std::isinf(a.sl2)) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: scale must be positive and below 2.3e38", who);
   if (window < 0) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: window=%d", who, window);
   if (batch->B == 0 || batch->rows == 0) return SPEC_OK;
   if ((rc = paged_rows_check(who, "d_q", cache, n_q_heads, d_q, q_stride))) return rc;
@@ -969,7 +970,6 @@ extern "C" int spec_paged_attention(void *hip_stream, const spec_paged_cache *ca
   a.q_stride = q_stride;
   a.out_stride = out_stride;
   a.window = endless ? 0 : window;
-  a.sl2 = scale * 1.4426950408889634f;
   a.part = (float *)d_workspace;
   a.ml = need ? a.part + (size_t)s.parts * cache->n_kv_heads * s.R * cache->head_dim : nullptr;
   a.chunk_min = s.whole ? 1 << 30 : PA_CHUNK_MIN;

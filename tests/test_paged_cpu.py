@@ -85,6 +85,12 @@ def test_attention_arguments(B):
     assert attend(B, cache(B), many) == B.ERR_CAPACITY
 
 
+def test_attention_scales_whose_power_of_two_form_is_infinite(B):
+    for scale in (2.4e38, 3.4e38):
+        assert attend(B, cache(B), batch(B), scale=scale) == B.ERR_INVALID_ARG
+    assert attend(B, cache(B), batch(B, B=0, rows=0), scale=2.3e38) == B.OK
+
+
 def test_logit_rules_arguments(B):
     def call(rules=None, logits=FAKE, dtype=B.DTYPE_F32, stride=1000, nB=2, s=3, V=1000, t=FAKE, out=FAKE + 64, **kw):
         r = rules if rules is not None else B.LogitRulesDesc(**kw)
