@@ -439,7 +439,7 @@ int spec_paged_append(void *hip_stream, const spec_paged_cache *cache, const spe
    (window = 0, or max_len and more: from 0 on).  Query head h reads key head h / (n_q_heads / n_kv_heads).  out = sum of softmax(scale * q.k)
    times v; a row that sees nothing is zeros, and what lies at positions that a row does not see never reaches it, be it
    infinite or NaN.  Scores, softmax and sums are fp32; softmax weights of 16-bit runs are rounded to the type once for the product
-   with the values.  n_q_heads a multiple of n_kv_heads; 0 < scale < 2.3e38.
+   with the values (fp16: a weight below 2^-21 of the row's largest by up to 2^-32 of that).  n_q_heads a multiple of n_kv_heads; 0 < scale < 2.3e38.
      d_q, d_out [rows][n_q_heads][head_dim], row strides in elements (alignment as above); rows that no sequence owns are
      left as they were in d_out.
      d_workspace: device scratch, 256-byte aligned, at least spec_paged_attention_workspace_bytes(); contents before and

@@ -200,6 +200,10 @@ template <> struct Mat<f16_t> {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_v){lo, hi}, f16x2_v));
   }
 };
+// log2 of the weight that the running maximum has.  fp16 has few small numbers: with the maximum's weight at 2^7 (2^15 where the maximum lags by 2^8), a weight
+// is rounded by more than 2^-11 of itself only below 2^-21 of the row's largest, by 2^-32 of the largest then.  With the maximum's at 1
+// 4000 positions of 2^-26 each counted for nothing.
+template <class T> constexpr float top_weight() { return std::is_same<T, f16_t>::value ? 7.f : 0.f; }
 
 // A lane's part of a step: its key rows of the two key tiles (KU units of 16 bytes each, units 4 kk + g), and 8 positions of
 // VE = HD / 16 values, as loaded.
@@ -381,7 +385,7 @@ __global__ __launch_bounds__(256, attend_resident(sizeof(T), HD, QT)) void k_pag
 #pragma unroll
         for (int ht = 0; ht < HT; ++ht) { acc[t][ht][0] *= corr; acc[t][ht][1] *= corr; acc[t][ht][2] *= corr; acc[t][ht][3] *= corr; }
       }
-      const float off = m[t] == -INFINITY ? 0.f : m[t] * a.sl2;
+      const float off = m[t] == -INFINITY ? 0.f : fmaf(m[t], a.sl2, -top_weight<T>());
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         sv[i] = __builtin_amdgcn_exp2f(fmaf(sv[i], a.sl2, -off));
@@ -535,7 +539,8 @@ __device__ __forceinline__ float max14(float top, const f32x16_v &x) {
 // every 16 keys, so a row's maximum takes one exchange.  Keys go straight to LDS, [key][unit of 16 bytes], a row's units exchanged by its number so
 // that reading one unit of 32 rows meets every bank; of values a thread loads 8 positions of 4 elements and turns them round on
 // the way to LDS.  The maximum follows the scores only when they have grown
-// by 2^8: weights up to 2^8 are as exact in 16 bits as weights up to 1, the sums are fp32, and most tiles then rescale nothing.
+// by 2^8: weights up to 2^8 are as exact in 16 bits as weights up to 1 (fp16: up to 2^15 as those up to 2^7), the sums are fp32, and most tiles
+// then rescale nothing.
 // Chunks of up to 2048 rows over 8192 positions, 32 heads over 8, bf16: 417 us (913 TFLOP/s), products busy 42 % of the clocks.
 constexpr int VALU = 0x2, MATRIX = 0x8, DS_READ = 0x100;  // kinds of instructions that sched_group_barrier tells apart
 constexpr int pc_lds(int NW) { return 4 * NW * 256 * 16; }
@@ -676,7 +681,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[j][e] *= corr;
     }
-    return m == -INFINITY ? 0.f : m * a.sl2;
+    return m == -INFINITY ? 0.f : fmaf(m, a.sl2, -top_weight<T>());
   };
   auto weights = [&](int y, float off) {  // of the 16 keys y of a step
     u32x4_v p;

@@ -1,4 +1,4 @@
-"""spec_paged_attention at the ends of the numbers' ranges: scores beyond fp32, the smallest scales."""
+"""spec_paged_attention at the ends of the numbers' ranges: scores beyond fp32, the smallest scales, weights far below the largest."""
 import pytest
 import torch
 
@@ -35,4 +35,29 @@ def test_the_smallest_scales_give_every_position_the_same_weight(dtype, rows, le
     q = c.rows_of(4)
     want, bound = ref.attention(c.k, c.v, c.table, c.batch, q, scale, 0)
     got = attend(c, q, scale=scale)
+    assert bool(((got - want).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("rows", [1, 9, 40, 130])
+@pytest.mark.parametrize("at", [0, 2500])
+def test_many_small_weights_beside_a_large_one(dtype, hd, rows, at):
+    """One position has a score 18 above all others (2^26 times their weight) and values of zero: what comes out is the others' 1e-5 of the
+    weight.  fp16 weights are held with the largest at 2^7 or more, so a rounding is 2^-25 / 2^7 of the largest weight at most where that is more
+    than 2^-11 of the weight itself."""
+    n, heads = 4000, 2
+    c = Case(dtype, heads, 1, hd, 64, [rows], [n + rows], seed=rows, extra_rows=0)
+    page, at_page = int(c.table[0, at // 64]), at % 64
+    c.k.zero_()
+    c.v.copy_((torch.rand(c.v.shape, generator=c.g) * 100 + 50).to(c.td))
+    c.k[page, at_page, 0, 0] = 18 * hd ** 0.5
+    c.v[page, at_page] = 0
+    q = c.rows_of(heads)
+    q[:, :, 0] = 1
+    want, bound = ref.attention(c.k, c.v, c.table, c.batch, q, hd ** -0.5, 0)
+    if dtype == "fp16":
+        bound = bound + 2.0 ** -32 * c.v.double().sum((0, 1, 2))
+    got = attend(c, q)
+    assert float((bound / want.abs()).max()) < 0.03
     assert bool(((got - want).abs() <= bound).all())
