@@ -156,9 +156,11 @@ void launch_process_logits(const void *logits, int dtype, int64_t row_stride, in
                            const int32_t *t, int t_stride, float *out, hipStream_t st) {
   LogitArgs a{logits, row_stride, s, V, 1024, s + 1, r, t, t_stride, out};
   if (!r.d_mask) a.r.mask_rows = 1;
-  // Every workgroup of a sequence goes through all its tokens.  Where these can be many, workgroups of 512 threads and pieces that leave 1024
-  // workgroups (24 sequences x 8 rows of 151936 logits, up to 16000 tokens: 52.8 us; 256 threads 61.0, pieces half as long 58.1); else 256
-  // threads and 2048 workgroups (64 x 4 rows of 50272, up to 1000 tokens: 19.9 us; 512 threads 26.6, 512 workgroups 25.2).
+  // Every workgroup of a sequence goes through all its tokens.  Where these can be many (their number is on the device: the list's room tells), workgroups of
+  // 512 threads and pieces that leave 1024 workgroups; else 256 threads and 2048 workgroups.  us with 512 and with 256 threads, bf16: 64 rows of 50272
+  // logits with 16000 tokens each 19.3 and 23.9, with 4000 13.2 and 14.6, with 1000 12.1 and 11.5; 24 x 8 rows of 151936 with 16000 46.5 and 48.4, with
+  // 500 38.4 and 37.9.  It does not pay where few sequences have several long rows: 8 x 4 rows of 151936 with 16000 17.3 and 15.0.  Pieces half as long:
+  // 24 x 8 fp32 rows of 151936 with up to 16000 tokens 53 -> 58.
   const bool many = r.d_tokens && r.tokens_stride > 4096;
   const int longest = r.n_bias ? 4096 : 8192, enough = many ? 1024 : 2048;
   while (a.piece < longest && (int64_t)B * ((V + 2 * a.piece - 1) / (2 * a.piece)) >= enough) a.piece *= 2;

@@ -708,8 +708,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_paged_chunk(AttendArgs a) {
   meet();
   int buf = 0;
   for (int ks0 = k_begin; ks0 < k_end; ks0 += KT, buf ^= 1) {
-    // The next tile's loads land while this one is worked on.  Behind the last tile they bring page 0's rows, which nothing reads: no branch
-    // keeps the address arithmetic from the products' shadow.
+    // The next tile's loads land while this one is worked on.  Behind the last tile they bring rows of the last position's page (page 0's if it
+    // is absent), which nothing reads: no branch keeps the address arithmetic from the products' shadow.
     fetch(ks0 + KT, pages, buf ^ 1);
     pages = pages_of(ks0 + 2 * KT);
     const int there = there_at(ks0 + KT);
@@ -870,7 +870,9 @@ struct Shape {
 };
 
 // Query rows of a tile: as few as hold a sequence's, since a tile reads the cache once for all of its rows.  Beyond 64 rows 128, or 256
-// where there are enough tiles of those.
+// where these make two rounds of workgroups and more.  us with 128 and with 256, bf16, 32 heads over 8: six sequences of 1000 rows (768 tiles of 256)
+// over up to 8192 positions 702 and 652 with heads of 128, 409 and 409 with heads of 64; one of 1500 (192 tiles) over 2048 positions
+// 68 and 66, 40 and 47; over 8192 253 and 219, 148 and 153.  So with few tiles heads of 64 gain from 128, heads of 128 would not need them.
 static Shape attend_shape(const spec_paged_cache *c, const spec_paged_batch *b, int n_q, int window) {
   Shape s{};
   const int64_t Hk = c->n_kv_heads, G = n_q / Hk, per = (int64_t)b->max_rows * G;
@@ -881,8 +883,12 @@ static Shape attend_shape(const spec_paged_cache *c, const spec_paged_batch *b, 
   s.align = s.qt < 8 ? 128 : s.R * 64 / c->head_dim;
   s.tiles = tiles(s.R);
   s.slots = std::max(1, 256 * attend_resident((int)dtype_bytes(c->dtype), c->head_dim, s.qt) / (int)Hk);
-  // What a tile can need at most decides whether any is cut, and so whether there is a second kernel, which costs 5 us and more even where it finds
-  // nothing to join: the steps of 1536 positions that four waves share cost less, and a chunk's longer ones where there are enough tiles.
+  // What a tile can need at most decides whether any is cut, and so whether there is a second kernel, which costs a launch and the search for its work
+  // even where it finds nothing to join.  us without cutting and with it, bf16, heads of 128.  One row of 64 sequences, 32 heads over 8: up to 1536 positions
+  // 67 and 77, up to 4096 164 and 174; of one sequence: 768 positions 11 and 11, 1536 18 and 12, 4096 43 and 16.  So many sequences pay 5 to 20 %
+  // for the second kernel, and few gain from it below the limit already.  Chunks of rows: 100 of one sequence over 448 positions 20 and 22, over
+  // 1024 35 and 27; 400 of eight sequences (832 tiles) over up to 2048 113 and 116; 300 of four (320 tiles) over up to 2048 71 and 104,
+  // over up to 3000 95 and 75.
   const int64_t span = window ? std::min<int64_t>(b->max_len, (int64_t)window + (s.R - 1) / G + 32) : b->max_len;
   s.whole = span <= (s.qt < 8 ? 1536 : s.tiles * Hk >= 256 ? 2048 : 512);
   s.units = s.tiles + (s.whole ? 0 : s.slots);
