@@ -447,7 +447,8 @@ int spec_paged_append(void *hip_stream, const spec_paged_cache *cache, const spe
    Other sequences of the pass decide, with their lengths and rows, whether and where a sequence's positions are cut into chunks.  So
    from one pass to another a row's result varies by the order of fp32 sums and, in 16-bit runs, by the rounding of its weights, which are
    rounded relative to the largest of their chunk so far; the same pass gives the same bits.
-   A row whose scores are all -infinity counts as one that sees nothing; where scale * q.k leaves fp32 otherwise, the row is NaN. */
+   A row whose scores are all -infinity counts as one that sees nothing; a row whose largest scale * q.k
+   leaves fp32 is NaN, and one with another that does can be. */
 int spec_paged_attention_workspace_bytes(const spec_paged_cache *cache, const spec_paged_batch *batch, int32_t n_q_heads,
                                          size_t *bytes);
 int spec_paged_attention(void *hip_stream, const spec_paged_cache *cache, const spec_paged_batch *batch, int32_t n_q_heads,
