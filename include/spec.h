@@ -455,6 +455,54 @@ int spec_paged_attention(void *hip_stream, const spec_paged_cache *cache, const 
                          const void *d_q, int64_t q_stride, float scale, int32_t window, void *d_workspace,
                          size_t workspace_bytes, void *d_out, int64_t out_stride);
 
+/* What a model does to queries and keys between the product and the cache, beyond spec_paged_append's rotation.  Per head, in this order:
+     y = x / sqrt(mean(x^2) + eps) * w, w = d_q_norm or d_k_norm ([head_dim], of the rows' type, 16-byte aligned; NULL: not normed)
+     the first rope_dim elements turn by the angles p * d_inv_freq[i] (as in spec_paged_append), in pairs i and i + rope_dim / 2, or, interleaved = 1,
+     2i and 2i + 1.
+   eps > 0 where there is a norm.  A NULL transform does nothing.  Sums of squares are 64 bits, products fp32, and one rounding ends it. */
+typedef struct {
+  const double *d_inv_freq; /* [rope_dim / 2]; may be NULL where rope_dim is 0 */
+  int32_t rope_dim;         /* a multiple of 16 up to head_dim                 */
+  int32_t interleaved;      /* 0 or 1                                          */
+  const void *d_q_norm, *d_k_norm;
+  double eps;
+} spec_head_transform;
+
+/* spec_paged_append for such models: rows, strides, dead rows, absent pages and what happens in place are as there; values are copied. */
+int spec_paged_append_normed(void *hip_stream, const spec_paged_cache *cache, const spec_paged_batch *batch,
+                             const spec_head_transform *transform, int32_t n_q_heads, const void *d_q, int64_t q_stride, const void *d_k,
+                             int64_t k_stride, const void *d_v, int64_t v_stride, void *d_q_out, int64_t q_out_stride);
+
+/* A paged cache of 8 bits under rows of 16: element i of position p of key head h in page g is the e4m3 code (OCP: up to 448, 0x7f and 0xff NaN, no
+   infinities) at d_k[g * page_stride + p * pos_stride + h * head_stride + i] times 2^(d_k_scale[(g * n_kv_heads + h) * page_size + p] - 127);
+   values likewise.  Strides in bytes, multiples of 16; d_k and d_v 16-byte aligned, the scales 8-byte aligned.  Sizes and limits otherwise as of
+   spec_paged_cache; dtype is that of the row-wise tensors, SPEC_DTYPE_BF16 or SPEC_DTYPE_F16 (SPEC_ERR_UNSUPPORTED for fp32).
+   Half the bytes of a cache of 16 bits and one more a head: twice the positions in the same memory, half the time of attention over long contexts.
+   An element is off by at most 1 / 16 of itself, or 2^-10 of its scale where that is more (2^-18 of the head's largest).  */
+typedef struct {
+  int32_t dtype;
+  int32_t head_dim, n_kv_heads, page_size, n_pages;
+  int64_t page_stride, pos_stride, head_stride; /* bytes */
+  uint8_t *d_k, *d_v;
+  uint8_t *d_k_scale, *d_v_scale; /* [n_pages][n_kv_heads][page_size] */
+} spec_paged_cache8;
+
+/* spec_paged8_append: spec_paged_append_normed into a cache of 8 bits.  Of a position's head y (keys in 64 bits up to the rounding, values as they
+   are): the scale is 2^e, e the least exponent, from -100 (bf16) or -15 (fp16) on, with max |y| <= 448 * 2^e; the codes are y / 2^e to nearest,
+   ties to even.  Magnitudes over the type's largest number of four bits (fp16: 61440) become that number; a head with a NaN, or with a magnitude that
+   the type rounds to infinity, is NaN throughout.  Queries stay in the rows' type.
+
+   spec_paged8_read: what the cache holds of the batch's rows, back in the rows' type (exactly): d_k, d_v [rows][n_kv_heads][head_dim], row strides in
+   elements, alignment as above; NULL: not wanted (not both).  Zeros where a page is absent; dead rows and rows that no sequence owns are left as they were.
+
+   spec_paged8_attention: spec_paged_attention over a cache of 8 bits; everything said there holds of the numbers that the cache stands for.
+   Scale bytes are what spec_paged8_append writes: one that takes a code out of the rows' type is not looked for.                    */
+int spec_paged8_append(void *hip_stream, const spec_paged_cache8 *cache, const spec_paged_batch *batch, const spec_head_transform *transform,
+                       int32_t n_q_heads, const void *d_q, int64_t q_stride, const void *d_k, int64_t k_stride, const void *d_v,
+                       int64_t v_stride, void *d_q_out, int64_t q_out_stride);
+int spec_paged8_read(void *hip_stream, const spec_paged_cache8 *cache, const spec_paged_batch *batch, void *d_k, int64_t k_stride, void *d_v,
+                     int64_t v_stride);
+
 /* Parity aids for the draft step (the call speculate(S, kv_SSM, s) of Alg. 1).
    spec_set_draft_logits: if d_logits is not NULL, every following spec_draft_step also writes the draft
    model's logits behind t_j -- the logits of the last token each sequence fed in -- as fp32 [B][vocab]

@@ -33,7 +33,7 @@ EXPORTS = ["spec_last_error", "spec_workspace_bytes", "spec_init", "spec_destroy
            "spec_set_draft_logits", "spec_read_proposals", "spec_greedy_accept_workspace_bytes", "spec_greedy_accept",
            "spec_greedy_accept_noalloc", "spec_set_gemm_tuning", "spec_read_saturation", "spec_sample_tokens",
            "spec_sample_accept", "spec_set_sampling", "spec_paged_append", "spec_paged_attention_workspace_bytes",
-           "spec_paged_attention", "spec_process_logits", "spec_set_logit_rules"]
+           "spec_paged_attention", "spec_paged_append_normed", "spec_paged8_append", "spec_paged8_read", "spec_process_logits", "spec_set_logit_rules"]
 KCLASS_NAMES = ["gemm_qkv", "gemm_o", "gemm_ffn_in", "gemm_ffn_out", "gemm_head", "attention", "norm", "other",
                 "draft_pass"]
 
@@ -62,6 +62,15 @@ class PagedCacheDesc(C.Structure):
 class PagedBatchDesc(C.Structure):
     _fields_ = [("B", C.c_int32), ("rows", C.c_int32), ("max_rows", C.c_int32), ("max_len", C.c_int32), ("d_row_start", C.c_void_p),
                 ("d_len", C.c_void_p), ("d_pages", C.c_void_p), ("pages_stride", C.c_int32)]
+
+
+class HeadTransformDesc(C.Structure):
+    _fields_ = [("d_inv_freq", C.c_void_p), ("rope_dim", C.c_int32), ("interleaved", C.c_int32), ("d_q_norm", C.c_void_p), ("d_k_norm", C.c_void_p),
+                ("eps", C.c_double)]
+
+
+class PagedCache8Desc(C.Structure):
+    _fields_ = PagedCacheDesc._fields_ + [("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p)]
 
 
 class LogitRulesDesc(C.Structure):
@@ -113,6 +122,10 @@ lib.spec_paged_append.argtypes = [_vp, C.POINTER(PagedCacheDesc), C.POINTER(Page
 lib.spec_paged_attention_workspace_bytes.argtypes = [C.POINTER(PagedCacheDesc), C.POINTER(PagedBatchDesc), _i32, C.POINTER(C.c_size_t)]
 lib.spec_paged_attention.argtypes = [_vp, C.POINTER(PagedCacheDesc), C.POINTER(PagedBatchDesc), _i32, _vp, _i64, C.c_float, _i32, _vp, C.c_size_t,
                                      _vp, _i64]
+_heads_args = [C.POINTER(PagedBatchDesc), C.POINTER(HeadTransformDesc), _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64]
+lib.spec_paged_append_normed.argtypes = [_vp, C.POINTER(PagedCacheDesc)] + _heads_args
+lib.spec_paged8_append.argtypes = [_vp, C.POINTER(PagedCache8Desc)] + _heads_args
+lib.spec_paged8_read.argtypes = [_vp, C.POINTER(PagedCache8Desc), C.POINTER(PagedBatchDesc), _vp, _i64, _vp, _i64]
 lib.spec_process_logits.argtypes = [_vp, _vp, _i32, _i64, _i32, _i32, _i32, C.POINTER(LogitRulesDesc), _vp, _vp]
 lib.spec_set_logit_rules.argtypes = [_vp, C.POINTER(LogitRulesDesc), _vp]
 lib.spec_set_attention_shape.argtypes = [_vp, _i32]
@@ -379,6 +392,96 @@ def spec_paged_append(cache, batch, q, k, v, inv_freq=None, out=None):
         rope, fp = 2 * inv_freq.shape[0], inv_freq.data_ptr()
     _call(cache.device, lib.spec_paged_append, cache.ref, batch._for(cache), nq, qp, qs, kp, ks, vp, vs, fp, rope, op, os_)
     return out if q is not None else None
+
+
+class HeadTransform:
+    """What a model does to queries and keys of each head in front of the cache: q_norm, k_norm [head_dim] of the rows' dtype (None: not normed)
+    with eps, and the rotation by position * inv_freq (float64 [rope_dim / 2], None: none) of pairs i, i + rope_dim / 2, or interleaved
+    ones, 2i, 2i + 1.  Device tensors, read when a call runs."""
+
+    def __init__(self, inv_freq=None, interleaved=False, q_norm=None, k_norm=None, eps=1e-6):
+        self.tensors = (inv_freq, q_norm, k_norm)  # must outlive their use
+        self.on = self.dtype = self.head_dim = None
+        for t in self.tensors:
+            if t is not None:
+                self.on = t.get_device() if self.on is None else self.on
+                assert t.get_device() == self.on >= 0 and t.dim() == 1 and t.is_contiguous()
+        assert inv_freq is None or inv_freq.dtype == torch.float64
+        for t in (q_norm, k_norm):
+            if t is not None:
+                assert self.dtype in (None, t.dtype) and self.head_dim in (None, t.shape[0]) and t.dtype in _DTYPE_OF
+                self.dtype, self.head_dim = t.dtype, t.shape[0]
+        p = lambda t: None if t is None else t.data_ptr()
+        self.desc = HeadTransformDesc(p(inv_freq), 0 if inv_freq is None else 2 * inv_freq.shape[0], int(bool(interleaved)), p(q_norm), p(k_norm), eps)
+        self.ref = C.byref(self.desc)
+
+
+def _append(fn, cache, batch, q, k, v, transform, out):
+    rows = batch.rows
+    kp, ks, kh = _heads(k, rows, cache)
+    vp, vs, vh = _heads(v, rows, cache)
+    assert kh == vh == cache.n_kv_heads
+    qp = op = ref = None
+    qs = os_ = nq = 0
+    if q is not None:
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        qp, qs, nq = _heads(q, rows, cache)
+        op, os_, no = _heads(out, rows, cache)
+        assert no == nq
+    if transform is not None:
+        assert transform.on in (None, cache.device.index) and transform.dtype in (None, cache.dtype) and transform.head_dim in (None, cache.head_dim)
+        ref = transform.ref
+    _call(cache.device, fn, cache.ref, batch._for(cache), ref, nq, qp, qs, kp, ks, vp, vs, op, os_)
+    return out if q is not None else None
+
+
+def spec_paged_append_normed(cache, batch, q, k, v, transform=None, out=None):
+    """spec_paged_append with a HeadTransform: q (None: keys and values only) and k normed and rotated, k and v into the pages.  -> out, the
+    transformed q (may be q itself)."""
+    return _append(lib.spec_paged_append_normed, cache, batch, q, k, v, transform, out)
+
+
+class PagedCache8:
+    """The keys and values of one layer in pages of 8 bits, under rows of `dtype` (bf16 or fp16): k, v [n_pages][page_size][n_kv_heads]
+    [head_dim] float8_e4m3fn (or their bytes, uint8), with strides as of PagedCache; k_scale, v_scale [n_pages][n_kv_heads][page_size] uint8."""
+
+    def __init__(self, k, v, k_scale, v_scale, dtype):
+        assert k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.dtype in (torch.float8_e4m3fn, torch.uint8)
+        assert k.stride() == v.stride() and k.stride(3) == 1
+        n, size, heads, hd = k.shape
+        for t in (k_scale, v_scale):
+            assert t.dtype == torch.uint8 and t.shape == (n, heads, size) and t.is_contiguous()
+        assert k.get_device() == v.get_device() == k_scale.get_device() == v_scale.get_device() >= 0
+        self.k, self.v, self.k_scale, self.v_scale, self.device = k, v, k_scale, v_scale, k.device  # must outlive their use
+        self.dtype, self.n_kv_heads, self.page_size, self.head_dim = dtype, heads, size, hd
+        self.desc = PagedCache8Desc(_DTYPE_OF[dtype], hd, heads, size, n, k.stride(0), k.stride(1), k.stride(2), k.data_ptr(), v.data_ptr(),
+                                    k_scale.data_ptr(), v_scale.data_ptr())
+        self.ref, self.scale = C.byref(self.desc), hd ** -0.5
+
+    @classmethod
+    def empty(cls, n_pages, page_size, n_kv_heads, head_dim, dtype, device="cuda:0"):
+        """A pool whose every position is zeros."""
+        pages = lambda: torch.zeros((n_pages, page_size, n_kv_heads, head_dim), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+        scales = lambda: torch.full((n_pages, n_kv_heads, page_size), 127, dtype=torch.uint8, device=device)
+        return cls(pages(), pages(), scales(), scales(), dtype)
+
+
+def spec_paged8_append(cache, batch, q, k, v, transform=None, out=None):
+    """spec_paged_append_normed into a PagedCache8."""
+    return _append(lib.spec_paged8_append, cache, batch, q, k, v, transform, out)
+
+
+def spec_paged8_read(cache, batch, k=None, v=None):
+    """What a PagedCache8 holds of the batch's rows -> (k, v) [rows][n_kv_heads][head_dim] of its dtype."""
+    shape = (batch.rows, cache.n_kv_heads, cache.head_dim)
+    k = torch.empty(shape, dtype=cache.dtype, device=cache.device) if k is None else k
+    v = torch.empty(shape, dtype=cache.dtype, device=cache.device) if v is None else v
+    kp, ks, kh = _heads(k, batch.rows, cache)
+    vp, vs, vh = _heads(v, batch.rows, cache)
+    assert kh == vh == cache.n_kv_heads
+    _call(cache.device, lib.spec_paged8_read, cache.ref, batch._for(cache), kp, ks, vp, vs)
+    return k, v
 
 
 def spec_paged_attention_workspace_bytes(cache, batch, n_q_heads):

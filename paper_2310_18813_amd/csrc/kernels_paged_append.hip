@@ -8,15 +8,14 @@
 
 namespace spec {
 
-int paged_args(const char *who, const spec_paged_cache *c, const spec_paged_batch *b, PagedArgs *out) {
-  if (!c || !b) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: cache or batch is null", who);
-  if (c->dtype < SPEC_DTYPE_F32 || c->dtype > SPEC_DTYPE_F16) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: unknown dtype %d", who, c->dtype);
+// bytes: of a cached element, which the strides count
+static int args_of(const char *who, const spec_paged_cache *c, int64_t bytes, const spec_paged_batch *b, PagedArgs *out) {
   if (c->head_dim != 64 && c->head_dim != 128) return fail_noctx(SPEC_ERR_UNSUPPORTED, "%s: head_dim %d is neither 64 nor 128", who, c->head_dim);
   if (c->page_size < 8 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)))
     return fail_noctx(SPEC_ERR_UNSUPPORTED, "%s: page_size %d is not a power of two from 8 to 1024", who, c->page_size);
   if (c->n_kv_heads < 1 || c->n_kv_heads > 65535 || c->n_pages < 1)
     return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: n_kv_heads=%d n_pages=%d", who, c->n_kv_heads, c->n_pages);
-  const int64_t unit = 16 / (int64_t)dtype_bytes(c->dtype);
+  const int64_t unit = 16 / bytes;
   const int64_t strides[3] = {c->page_stride, c->pos_stride, c->head_stride};
   for (int64_t s : strides)
     if (s < 0 || s % unit) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: cache strides must be non-negative multiples of 16 bytes", who);
@@ -41,7 +40,27 @@ int paged_args(const char *who, const spec_paged_cache *c, const spec_paged_batc
   *out = PagedArgs{(unsigned char *)c->d_k, (unsigned char *)c->d_v, (uint32_t)(c->page_stride / unit), (uint32_t)(c->pos_stride / unit),
                    (uint32_t)(c->head_stride / unit), c->n_pages,
                    __builtin_ctz(c->page_size), c->n_kv_heads, b->B, b->rows, b->max_rows, b->max_len, b->d_row_start, b->d_len, b->d_pages,
-                   b->pages_stride};
+                   b->pages_stride, nullptr, nullptr};
+  return SPEC_OK;
+}
+
+int paged_args(const char *who, const spec_paged_cache *c, const spec_paged_batch *b, PagedArgs *out) {
+  if (!c || !b) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: cache or batch is null", who);
+  if (c->dtype < SPEC_DTYPE_F32 || c->dtype > SPEC_DTYPE_F16) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: unknown dtype %d", who, c->dtype);
+  return args_of(who, c, (int64_t)dtype_bytes(c->dtype), b, out);
+}
+
+int paged8_args(const char *who, const spec_paged_cache8 *c, const spec_paged_batch *b, spec_paged_cache *as, PagedArgs *out) {
+  if (!c || !b) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: cache or batch is null", who);
+  if (c->dtype < SPEC_DTYPE_F32 || c->dtype > SPEC_DTYPE_F16) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: unknown dtype %d", who, c->dtype);
+  if (c->dtype == SPEC_DTYPE_F32) return fail_noctx(SPEC_ERR_UNSUPPORTED, "%s: rows of fp32 have no cache of 8 bits", who);
+  *as = spec_paged_cache{c->dtype, c->head_dim, c->n_kv_heads, c->page_size, c->n_pages, c->page_stride, c->pos_stride, c->head_stride, c->d_k, c->d_v};
+  const int rc = args_of(who, as, 1, b, out);
+  if (rc) return rc;
+  if (!c->d_k_scale || !c->d_v_scale || ((uintptr_t)c->d_k_scale & 7) || ((uintptr_t)c->d_v_scale & 7))
+    return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: the scales must be set and 8-byte aligned", who);
+  out->k_scale = c->d_k_scale;
+  out->v_scale = c->d_v_scale;
   return SPEC_OK;
 }
 
@@ -53,8 +72,6 @@ int paged_rows_check(const char *who, const char *what, const spec_paged_cache *
   return SPEC_OK;
 }
 
-typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_v;
-
 struct AppendArgs {
   PagedArgs p;
   const unsigned char *q, *k, *v;
@@ -63,37 +80,6 @@ struct AppendArgs {
   const double *inv_freq;
   int n_q, half;  // query heads; half the rotated elements
 };
-
-// 16 bytes as numbers and back
-template <class T> struct Unit {
-  static constexpr int E = 16 / sizeof(T);
-  static __device__ __forceinline__ void load(const u32x4_v &x, float (&f)[E]) {
-    T t[E];
-    __builtin_memcpy(t, &x, 16);
-#pragma unroll
-    for (int i = 0; i < E; ++i) f[i] = Conv<T>::ld(t, i);
-  }
-  static __device__ __forceinline__ u32x4_v store(const float (&f)[E]) {
-    T t[E];
-#pragma unroll
-    for (int i = 0; i < E; ++i) Conv<T>::st(t, i, f[i]);
-    u32x4_v x;
-    __builtin_memcpy(&x, t, 16);
-    return x;
-  }
-};
-
-// The sequence of a row: how many sequences end at or before it.  A wave reads the boundaries together.
-__device__ __forceinline__ int row_sequence(const PagedArgs &a, int row) {
-  if (!a.row_start) return row / (a.rows / a.B);
-  int b = 0;
-  for (int k0 = 0; k0 < a.B; k0 += 64) {
-    const int k = k0 + (int)(threadIdx.x & 63);
-    const bool before = k < a.B && a.row_start[min(k, a.B - 1) + 1] <= row;
-    b += __popcll(__ballot(before));
-  }
-  return b;
-}
 
 // A workgroup takes one row and 256 of its items; an item is two units of 16 bytes of a head: a rotated pair of them, or two that pass.
 template <class T, int HD>

@@ -29,7 +29,6 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2_v;
 typedef __attribute__((ext_vector_type(2))) _Float16 f16x2_v;
 typedef __attribute__((ext_vector_type(2))) float f32x2_v;
 typedef __attribute__((ext_vector_type(4))) float f32x4_v;
-typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_v;
 
 constexpr int PA_CHUNK_MIN = 512; // positions of the shortest chunk
 constexpr int PA_WAVES = 4;
