@@ -382,6 +382,37 @@ int spec_process_logits(void *hip_stream, const void *d_logits, int32_t dtype, i
                         int32_t vocab, const spec_logit_rules *rules, const int32_t *d_proposals, float *d_out);
 int spec_set_logit_rules(spec_ctx *ctx, const spec_logit_rules *rules, float *d_target_logits);
 
+/* What else a request asks of its tokens: temperature, top-k, top-p and min-p, each sequence its own.  Tokens of a row come in the order of their
+   logits, the largest first, equal ones by their ids; NaN counts as -infinity, and tokens at -infinity are never kept.  With m the largest logit,
+   x = (z - m) / T and w = e^x, T = d_temperature[b], kept are in this order
+     T <= 0 or NaN: the first token alone (greedy)
+     of all tokens the first d_top_k[b] (<= 0: all)
+     of these the smallest number of first ones whose weights add up to d_top_p[b] times the weights of these or more (>= 1 or NaN: all)
+     of these the tokens with w >= d_min_p[b] (<= 0 or NaN: all; > 1 counts as 1)
+   The first token is always kept.  NULL leaves a rule out (T = 1).  An infinite temperature gives every token the same weight; where the largest logit is
+   infinite, the infinite ones share the weight. */
+typedef struct {
+  const float *d_temperature; /* [B] */
+  const int32_t *d_top_k;     /* [B] */
+  const float *d_top_p, *d_min_p; /* [B] */
+} spec_sampling_rules;
+
+/* spec_truncate_logits: the rules on d_logits, [B][s+1] rows as of spec_process_logits (any type, padded).
+     d_out [B][s+1][vocab] fp32 or NULL: x of the tokens that are kept, -infinity for the others: what spec_sample_accept and spec_sample_tokens take with
+     temperature 1 (target and draft rows alike), and what the round's acceptance is then exact for.  May be d_logits itself where the type
+     is fp32 and row_stride = vocab.
+     d_tokens [B][s+1] or NULL (not both): a draw from the kept tokens with d_uniforms [B][s+1], numbers in [0, 1): the lowest id whose cumulative weight
+     exceeds u times the sum.  A row without any token above -infinity yields -infinity throughout and token 0.
+     d_workspace: scratch of spec_truncate_logits_workspace_bytes() (which may be 0: then NULL), 256-byte aligned; calls that may overlap need one each.
+   Weights are whole multiples of 2^-50 (2^(bits - 62) with vocabularies of more than 2^12 tokens, of up to 2^bits) and computed in 64 bits, so
+   their sums are exact and the same in whatever order: which tokens are kept and drawn differs from the definition only where a sum comes within
+   some 10^-12 of its limit.  Enqueues on hip_stream (NULL = the default stream), needs no context, does not wait.
+   s <= 15, B <= 65535, vocab <= 2^28 (SPEC_ERR_CAPACITY). */
+int spec_truncate_logits_workspace_bytes(int32_t B, int32_t s, int32_t vocab, size_t *bytes);
+int spec_truncate_logits(void *hip_stream, const void *d_logits, int32_t dtype, int64_t row_stride, int32_t B, int32_t s, int32_t vocab,
+                         const spec_sampling_rules *rules, const float *d_uniforms, void *d_workspace, size_t workspace_bytes, float *d_out,
+                         int32_t *d_tokens);
+
 /* Operators for a caller that runs the target model itself over a paged cache: what its verification pass needs between
    the products, beside the acceptance rules above.  None needs a context; all enqueue on hip_stream (NULL = the default
    stream) and return without waiting; lengths, pages and rows are read on the device, so a call can be captured into a

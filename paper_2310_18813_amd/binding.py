@@ -33,7 +33,8 @@ EXPORTS = ["spec_last_error", "spec_workspace_bytes", "spec_init", "spec_destroy
            "spec_set_draft_logits", "spec_read_proposals", "spec_greedy_accept_workspace_bytes", "spec_greedy_accept",
            "spec_greedy_accept_noalloc", "spec_set_gemm_tuning", "spec_read_saturation", "spec_sample_tokens",
            "spec_sample_accept", "spec_set_sampling", "spec_paged_append", "spec_paged_attention_workspace_bytes",
-           "spec_paged_attention", "spec_paged_append_normed", "spec_paged8_append", "spec_paged8_read", "spec_process_logits", "spec_set_logit_rules"]
+           "spec_paged_attention", "spec_paged_append_normed", "spec_paged8_append", "spec_paged8_read", "spec_process_logits", "spec_set_logit_rules",
+           "spec_truncate_logits_workspace_bytes", "spec_truncate_logits"]
 KCLASS_NAMES = ["gemm_qkv", "gemm_o", "gemm_ffn_in", "gemm_ffn_out", "gemm_head", "attention", "norm", "other",
                 "draft_pass"]
 
@@ -77,6 +78,10 @@ class LogitRulesDesc(C.Structure):
     _fields_ = [("d_tokens", C.c_void_p), ("tokens_stride", C.c_int64), ("d_prompt_len", C.c_void_p), ("d_len", C.c_void_p),
                 ("d_repetition", C.c_void_p), ("d_frequency", C.c_void_p), ("d_presence", C.c_void_p), ("d_bias_ids", C.c_void_p),
                 ("d_bias", C.c_void_p), ("n_bias", C.c_int32), ("d_mask", C.c_void_p), ("mask_rows", C.c_int32)]
+
+
+class SamplingRulesDesc(C.Structure):
+    _fields_ = [("d_temperature", C.c_void_p), ("d_top_k", C.c_void_p), ("d_top_p", C.c_void_p), ("d_min_p", C.c_void_p)]
 
 
 _vp, _i32, _i32p, _f32p, _i64p = C.c_void_p, C.c_int32, C.POINTER(C.c_int32), C.POINTER(C.c_float), C.POINTER(C.c_int64)
@@ -127,6 +132,8 @@ lib.spec_paged_append_normed.argtypes = [_vp, C.POINTER(PagedCacheDesc)] + _head
 lib.spec_paged8_append.argtypes = [_vp, C.POINTER(PagedCache8Desc)] + _heads_args
 lib.spec_paged8_read.argtypes = [_vp, C.POINTER(PagedCache8Desc), C.POINTER(PagedBatchDesc), _vp, _i64, _vp, _i64]
 lib.spec_process_logits.argtypes = [_vp, _vp, _i32, _i64, _i32, _i32, _i32, C.POINTER(LogitRulesDesc), _vp, _vp]
+lib.spec_truncate_logits_workspace_bytes.argtypes = [_i32, _i32, _i32, C.POINTER(C.c_size_t)]
+lib.spec_truncate_logits.argtypes = [_vp, _vp, _i32, _i64, _i32, _i32, _i32, C.POINTER(SamplingRulesDesc), _vp, _vp, C.c_size_t, _vp, _vp]
 lib.spec_set_logit_rules.argtypes = [_vp, C.POINTER(LogitRulesDesc), _vp]
 lib.spec_set_attention_shape.argtypes = [_vp, _i32]
 lib.spec_set_gemm_tuning.argtypes = [_vp, _i32, _i32, _i32]
@@ -287,14 +294,20 @@ class LogitRules:
         self.ref = C.byref(self.desc)
 
 
+def _logit_rows(logits):
+    """-> (shape, row stride, device index) of logits [B][s+1][V] whose rows may be padded."""
+    nB, q, V = logits.shape
+    s0, s1, s2 = logits.stride()
+    row = s1 if q > 1 else s0 if nB > 1 else V
+    assert (s2 == 1 or V < 2) and (nB < 2 or s0 == q * row)
+    return logits.shape, row, logits.get_device()
+
+
 def spec_process_logits(logits, rules, proposals=None, out=None):
     """logits [B][s+1][V] (fp32, bf16 or fp16, rows may be padded), proposals [B][s] int32 or None -> out [B][s+1][V] fp32, which
     may be logits itself."""
-    shape = nB, q, V = logits.shape
-    s0, s1, s2 = logits.stride()
-    row = s1 if q > 1 else s0 if nB > 1 else V
-    assert s2 == 1 and (nB < 2 or s0 == q * row)
-    on = logits.get_device()
+    shape, row, on = _logit_rows(logits)
+    nB, q, V = shape
     assert on >= 0 and rules.on in (None, on)
     assert rules.B is None or rules.B == nB
     assert rules.mask_words is None or rules.mask_words == (V + 31) // 32
@@ -307,6 +320,57 @@ def spec_process_logits(logits, rules, proposals=None, out=None):
     assert out.dtype is torch.float32 and out.shape == shape and out.is_contiguous() and out.get_device() == on
     _call(logits.device, lib.spec_process_logits, logits.data_ptr(), _DTYPE_OF[logits.dtype], row, nB, q - 1, V, rules.ref, pp, out.data_ptr())
     return out
+
+
+class SamplingRules:
+    """What each sequence asks of its tokens, device tensors [B] (None: not that rule): temperature, top_p, min_p fp32, top_k int32.  Read when a call
+    runs: a program may update them in place between calls."""
+
+    def __init__(self, temperature=None, top_k=None, top_p=None, min_p=None):
+        self.tensors = (temperature, top_k, top_p, min_p)  # must outlive their use
+        self.B = self.on = None
+        for t in self.tensors:
+            if t is not None:
+                self.on = t.get_device() if self.on is None else self.on
+                self.B = t.shape[0] if self.B is None else self.B
+                assert t.get_device() == self.on >= 0 and t.dim() == 1 and t.is_contiguous() and t.shape[0] == self.B
+                assert t.dtype == (torch.int32 if t is top_k else torch.float32)
+        self.desc = SamplingRulesDesc(*(None if t is None else t.data_ptr() for t in self.tensors))
+        self.ref = C.byref(self.desc)
+
+
+def spec_truncate_logits_workspace_bytes(nB, s, vocab):
+    n = C.c_size_t(0)
+    _check(lib.spec_truncate_logits_workspace_bytes(nB, s, vocab, C.byref(n)))
+    return n.value
+
+
+def spec_truncate_logits(logits, rules, uniforms=None, out=None, tokens=None, workspace=None, want_logits=True):
+    """logits [B][s+1][V] (fp32, bf16 or fp16, rows may be padded), a SamplingRules -> (out [B][s+1][V] fp32: log weights relative to the
+    row's largest, -inf where a token is not kept; tokens [B][s+1] int32 drawn with uniforms [B][s+1] fp32).  out may be logits itself; None without
+    want_logits, as tokens without uniforms.  workspace: a uint8 tensor of spec_truncate_logits_workspace_bytes() (allocated if None)."""
+    shape, row, on = _logit_rows(logits)
+    nB, q, V = shape
+    assert on >= 0 and rules.on in (None, on) and rules.B in (None, nB)
+    if out is None and want_logits:
+        out = torch.empty(shape, dtype=torch.float32, device=logits.device)
+    if out is not None:
+        assert out.dtype is torch.float32 and out.shape == shape and out.is_contiguous() and out.get_device() == on
+    up = tp = None
+    if uniforms is not None:
+        assert uniforms.dtype is torch.float32 and uniforms.shape == (nB, q) and uniforms.is_contiguous() and uniforms.get_device() == on
+        if tokens is None:
+            tokens = torch.empty((nB, q), dtype=torch.int32, device=logits.device)
+        assert tokens.dtype is torch.int32 and tokens.shape == (nB, q) and tokens.is_contiguous() and tokens.get_device() == on
+        up, tp = uniforms.data_ptr(), tokens.data_ptr()
+    else:
+        assert tokens is None
+    if workspace is None:
+        workspace = torch.empty(spec_truncate_logits_workspace_bytes(nB, q - 1, V), dtype=torch.uint8, device=logits.device)
+    assert workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.get_device() == on
+    _call(logits.device, lib.spec_truncate_logits, logits.data_ptr(), _DTYPE_OF[logits.dtype], row, nB, q - 1, V, rules.ref, up,
+          workspace.data_ptr() or None, workspace.numel(), None if out is None else out.data_ptr(), tp)
+    return out, tokens
 
 
 _DTYPE_OF = {v: k for k, v in TORCH_DTYPE.items()}

@@ -1,0 +1,263 @@
+"""spec_truncate_logits against its definition in 64 bits: every rule by itself and all together, types, vocabularies from one token on, ties, rows that
+are flat, masked or not finite, in place, padded, on another stream and in a graph; and the acceptance rules behind it."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+NEAR = 1e-10  # how near a sum may be to its limit for either side to be right: weights are off by 2^-44 of the largest and 3e-13 of themselves
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2310_18813_amd import binding
+    return binding
+
+
+def definition(z, T, k, p, floor):
+    """-> (order of the kept tokens, fewest and most of them, x)"""
+    z = np.where(np.isnan(z), -np.inf, z.astype(np.float64))
+    alive = int((z > -np.inf).sum())
+    if alive == 0:
+        return np.zeros(0, dtype=np.int64), 0, 0, np.zeros_like(z)
+    order = np.argsort(-z, kind="stable")[:alive]
+    m = z[order[0]]
+    if not T > 0:
+        return order[:1], 1, 1, np.zeros_like(z)
+    with np.errstate(invalid="ignore", over="ignore"):
+        x = np.where(z == m, 0.0, (z - m) / T) if not math.isinf(T) else np.where((z == m) | (np.isfinite(z) & np.isfinite(m)), 0.0, -np.inf)
+    w = np.exp(x[order])
+    n = min(k, alive) if k > 0 else alive
+    low = high = n
+    if p < 1:
+        mass = np.cumsum(w[:n])
+        low, high = (min(n, 1 + int((mass < max(p, 0.0) * mass[-1] * (1 + d)).sum())) for d in (-NEAR, NEAR))
+    if floor > 0:
+        at_least = [max(1, int((w >= min(floor, 1.0) * (1 + d)).sum())) if min(floor, 1.0) < 1 else int((w >= 1).sum()) for d in (NEAR, -NEAR)]
+        low, high = min(low, at_least[0]), min(high, at_least[1])
+    return order, low, high, x
+
+
+def check(logits, out, T=None, k=None, p=None, floor=None, u=None, tokens=None):
+    logits = logits.double().cpu().numpy()
+    out = None if out is None else out.double().cpu().numpy()
+    n_kept = []
+    for b in range(logits.shape[0]):
+        t, kk, pp, fl = (d if r is None else float(r[b]) for r, d in ((T, 1.0), (k, 0), (p, 1.0), (floor, 0.0)))
+        for j in range(logits.shape[1]):
+            order, low, high, x = definition(logits[b, j], t, int(kk), pp, fl)
+            n = high
+            if out is not None:
+                # (a token that is kept and whose x leaves fp32 is -infinity as well)
+                got = np.flatnonzero(out[b, j] > -np.inf)
+                fits = [m for m in range(low, high + 1) if np.array_equal(np.sort(order[:m][x[order[:m]] > -3.4e38]), got)]
+                assert fits, (b, j, t, kk, pp, fl, len(got), low, high)
+                n = fits[-1]
+                # a difference, rounded, and a quotient, rounded: 2^-24 each
+                assert (np.abs(out[b, j, got] - x[got]) <= 2.0 ** -22 * np.abs(x[got]) + 1e-45).all()
+            n_kept.append(n)
+            if tokens is not None:
+                token = int(tokens[b, j])
+                if n == 0:
+                    assert token == 0
+                    continue
+                ids = np.sort(order[:n])
+                c = np.cumsum(np.exp(x[ids]))
+                at, uu = np.searchsorted(ids, token), float(u[b, j])
+                assert at < n and ids[at] == token
+                assert c[at] > uu * c[-1] * (1 - NEAR) and (at == 0 or c[at - 1] <= uu * c[-1] * (1 + NEAR)), (b, j, token)
+    return n_kept
+
+
+def rules_of(B, **kw):
+    types = dict(temperature=torch.float32, top_k=torch.int32, top_p=torch.float32, min_p=torch.float32)
+    on = {n: torch.tensor(v, dtype=types[n], device=DEV) for n, v in kw.items() if v is not None}
+    return B.SamplingRules(**on), {n: on[n].cpu() if n in on else None for n in types}
+
+
+def run(B, logits, uniforms=True, seed=0, **kw):
+    rules, on = rules_of(B, **kw)
+    u = torch.rand(logits.shape[:2], generator=torch.Generator().manual_seed(seed + 3))
+    out, tokens = B.spec_truncate_logits(logits, rules, uniforms=u.to(DEV) if uniforms else None)
+    return check(logits, out, on["temperature"], on["top_k"], on["top_p"], on["min_p"], u, tokens.cpu() if uniforms else None)
+
+
+def logits_of(nB, q, V, td=torch.float32, seed=0, size=3.0):
+    g = torch.Generator().manual_seed(seed + 11)
+    return (size * torch.randn((nB, q, V), generator=g)).to(td).to(DEV)
+
+
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+
+
+@pytest.mark.parametrize("td", TYPES)
+@pytest.mark.parametrize("V", [1, 2, 5, 63, 257, 1000, 4095, 8192, 8193, 9001, 32000])
+def test_all_rules_over_vocabularies(B, V, td):
+    kept = run(B, logits_of(6, 2, V, td, seed=V), temperature=[1.0, 0.7, 0.0, 1.5, 0.2, math.inf], top_k=[0, 50, 7, 400, 1, 30],
+               top_p=[0.9, 0.8, 0.5, 0.999, 1.0, 0.6], min_p=[0.0, 0.02, 0.3, 0.001, 0.0, 0.0])
+    assert kept[4] == kept[5] == 1 and len(kept) == 12
+
+
+@pytest.mark.parametrize("td", TYPES)
+def test_each_rule_by_itself(B, td):
+    z = logits_of(4, 1, 5003, td, seed=3)
+    assert run(B, z) == [5003] * 4
+    assert run(B, z, top_k=[-3, 1, 5002, 5003]) == [5003, 1, 5002, 5003]
+    assert run(B, z, top_k=[2, 64, 65, 1 << 30]) == [2, 64, 65, 5003]
+    run(B, z, top_p=[0.0, 1e-9, 0.5, 0.9999])
+    assert run(B, z, top_p=[-1.0, 1.0, 2.0, math.nan])[1:] == [5003] * 3
+    run(B, z, min_p=[0.5, 1e-3, 1e-20, 1e-38])
+    kept = run(B, z, min_p=[0.0, -1.0, math.nan, 2.0])
+    assert kept[:3] == [5003] * 3
+    run(B, z, temperature=[1e-30, 3.0, 100.0, 1e30])
+    assert run(B, z, temperature=[0.0, -1.0, math.nan, 0.0]) == [1] * 4
+
+
+@pytest.mark.parametrize("V", [1000, 20000])
+def test_ties_go_to_the_lowest_ids(B, V):
+    """Few distinct logits: the border lies among thousands of equal ones."""
+    g = torch.Generator().manual_seed(5)
+    z = torch.randint(0, 5, (5, 2, V), generator=g).float().to(DEV)
+    run(B, z, top_k=[3, V // 3, V - 7, V // 2, 1], top_p=[1.0, 0.97, 0.5, 1.0, 0.5])
+    flat = torch.full((5, 1, V), -2.5, device=DEV)
+    assert run(B, flat, top_k=[1, 64, 65, V - 1, 0]) == [1, 64, 65, V - 1, V]
+    assert run(B, flat, top_p=[0.25, 0.5, 0.75, 0.0, 1.0]) == [V // 4, V // 2, 3 * V // 4, 1, V]
+    zeros = torch.zeros((1, 1, V), device=DEV)
+    zeros[..., ::2] = -0.0
+    assert run(B, zeros, top_k=[V // 2 + 3]) == [V // 2 + 3]
+
+
+def test_narrow_and_wide_rows(B):
+    """Logits that differ in their last bits alone, steep rows, and rows that reach over all of fp32."""
+    V = 12001
+    g = torch.Generator().manual_seed(6)
+    near = 1.0 + torch.randint(0, 300, (3, 1, V), generator=g).float() * 2.0 ** -23
+    run(B, near.to(DEV), top_k=[5000, 77, 0], top_p=[1.0, 0.6, 0.3])
+    wide = torch.randn((3, 1, V), generator=g) * 1e38
+    run(B, wide.to(DEV), temperature=[1.0, 1e38, math.inf], top_k=[5000, 1000, 0], top_p=[1.0, 0.9, 0.3])
+    steep = torch.randn((2, 1, V), generator=g) * 200
+    run(B, steep.to(DEV), top_k=[6000, 6000], top_p=[1.0, 0.999])
+
+
+def test_infinities_nan_and_masked_rows(B):
+    V, inf = 3001, math.inf
+    z = logits_of(8, 1, V, seed=8).cpu()
+    z[0] = -inf
+    z[1] = math.nan
+    z[2, 0, 5:] = -inf                      # five tokens, more asked for
+    z[3, 0, ::2] = math.nan
+    z[4, 0, [10, 2000, 77]] = inf           # they share the weight
+    z[5, 0, [10, 2000]] = inf
+    z[6, 0, :] = -inf
+    z[6, 0, 2999] = -3e38
+    z[7, 0, :1500] = -inf
+    got = run(B, z.to(DEV), top_k=[10, 10, 10, 10, 2, 0, 10, 100], top_p=[0.9, 0.9, 1.0, 0.9, 1.0, 0.6, 0.9, 1.0])
+    assert got[:3] == [0, 0, 5] and got[4:8] == [2, 2, 1, 100]
+    got = run(B, z.to(DEV), temperature=[0.0, 0.0, 0.0, 0.0, 0.0, 0.5, inf, inf], min_p=[0.1] * 8)
+    assert got[:3] == [0, 0, 1] and got[3:5] == [1, 1] and got[5] == 2 and got[6] == 1 and got[7] == 1501
+
+
+def test_draws_at_the_ends_of_the_uniform_numbers(B):
+    z = logits_of(4, 1, 9003, seed=9)
+    z[:, :, 0] = -math.inf
+    rules, on = rules_of(B, top_p=[0.9, 1.0, 0.5, 1.0], top_k=[0, 0, 0, 1])
+    for u in (0.0, 1 - 2.0 ** -24, 2.0 ** -149, 0.5):
+        us = torch.full((4, 1), u)
+        out, tokens = B.spec_truncate_logits(z, rules, uniforms=us.to(DEV))
+        check(z, out, p=on["top_p"], k=on["top_k"], u=us, tokens=tokens.cpu())
+
+
+def test_tokens_alone_logits_alone_in_place_and_padded(B):
+    V = 10004
+    big = torch.zeros((3, 2, V + 20), device=DEV)
+    big[..., :V] = logits_of(3, 2, V, seed=12)
+    z, dense = big[..., :V], big[..., :V].contiguous()
+    rules, _ = rules_of(B, temperature=[0.8, 0.0, 1.1], top_k=[40, 5, 0], top_p=[0.9, 0.9, 0.7], min_p=[0.0, 0.1, 0.01])
+    u = torch.rand((3, 2), device=DEV)
+    out, tokens = B.spec_truncate_logits(z, rules, uniforms=u)
+    assert torch.equal(B.spec_truncate_logits(dense, rules)[0], out)
+    none, alone = B.spec_truncate_logits(z, rules, uniforms=u, want_logits=False)
+    assert none is None and torch.equal(alone, tokens)
+    mine = dense.clone()
+    got, t = B.spec_truncate_logits(mine, rules, uniforms=u, out=mine)
+    assert got is mine and torch.equal(mine, out) and torch.equal(t, tokens)
+    mine = dense.clone()
+    B.spec_truncate_logits(mine, rules, out=mine)
+    assert torch.equal(mine, out)
+    odd = torch.zeros(3 * 2 * V + 1, device=DEV)[1:].view(3, 2, V)  # not 16-byte aligned
+    odd.copy_(dense)
+    assert torch.equal(B.spec_truncate_logits(odd, rules)[0], out)
+    assert (big[..., V:] == 0).all()
+
+
+def test_the_same_bits_every_time_and_on_another_stream(B):
+    z = logits_of(40, 2, 20011, torch.bfloat16, seed=13)
+    rules, _ = rules_of(B, top_k=[0, 900] * 20, top_p=[0.95, 0.9] * 20)
+    u = torch.rand((40, 2), device=DEV)
+    want, tokens = B.spec_truncate_logits(z, rules, uniforms=u)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        again = [B.spec_truncate_logits(z, rules, uniforms=u) for _ in range(3)]
+    s.synchronize()
+    for o, t in again:
+        assert torch.equal(o, want) and torch.equal(t, tokens)
+
+
+def test_replayed_graph_follows_logits_and_rules(B):
+    V = 16000
+    z, u = logits_of(4, 2, V, seed=14), torch.rand((4, 2), device=DEV)
+    rules, _ = rules_of(B, temperature=[0.8, 0.0, 1.1, 1.0], top_k=[40, 5, 0, 0], top_p=[0.9, 0.9, 0.7, 1.0])
+    out, tokens = torch.empty_like(z), torch.empty((4, 2), dtype=torch.int32, device=DEV)
+    space = torch.empty(B.spec_truncate_logits_workspace_bytes(4, 1, V), dtype=torch.uint8, device=DEV)
+    g, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s), torch.cuda.graph(g, stream=s):
+        B.spec_truncate_logits(z, rules, uniforms=u, out=out, tokens=tokens, workspace=space)
+    for step in range(4):
+        z.copy_(logits_of(4, 2, V, seed=20 + step))
+        u.copy_(torch.rand((4, 2)))
+        rules.tensors[0].copy_(rules.tensors[0].roll(1))
+        rules.tensors[1].add_(step)
+        want, wt = B.spec_truncate_logits(z, rules, uniforms=u)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(tokens, wt)
+
+
+def test_the_draw_is_that_of_sample_tokens_behind_it(B):
+    """Two ways to one token: the draw here, and spec_sample_tokens on what is kept (fp32 sums: another token where u is within 1e-5 of a border)."""
+    z, V = logits_of(64, 1, 32000, seed=15), 32000
+    rules, _ = rules_of(B, top_k=[50] * 64, top_p=[0.9] * 64)
+    u = torch.rand((64, 1), generator=torch.Generator().manual_seed(4)).to(DEV)
+    out, tokens = B.spec_truncate_logits(z, rules, uniforms=u)
+    other = B.spec_sample_tokens(out.view(64, V), u.view(64), 1.0).view(64, 1)
+    w = torch.exp(out.double())
+    c = w.cumsum(-1) / w.sum(-1, keepdim=True)
+    near = ((c - u[..., None].double()).abs().amin(-1) < 1e-5)
+    assert ((other == tokens) | near).all() and int((other == tokens).sum()) > 60
+
+
+def test_a_round_of_mixed_requests(B):
+    """Greedy and sampled sequences in one round: rules on target and draft rows, then the acceptance.  A greedy sequence gets the greedy round, a sampled
+    one never a token outside of what its target row keeps."""
+    nB, s, V = 24, 3, 9000
+    target, draft = logits_of(nB, s + 1, V, seed=16), logits_of(s, nB, V, seed=17).transpose(0, 1).contiguous()
+    draft = 0.7 * draft + target[:, :s]
+    T = [0.0 if b % 3 == 0 else 0.9 for b in range(nB)]
+    rules, _ = rules_of(B, temperature=T, top_k=[40] * nB, top_p=[0.9] * nB)
+    u = torch.rand((nB, s + 1, 3), generator=torch.Generator().manual_seed(5)).to(DEV)
+    q, proposals = B.spec_truncate_logits(draft, rules, uniforms=u[:, :s, 0].contiguous())
+    p, _ = B.spec_truncate_logits(target, rules)
+    chosen, accepted, emitted = B.spec_sample_accept(p, q.transpose(0, 1).contiguous(), proposals, u, 1.0)
+    ga, ge = B.spec_greedy_accept(target, proposals)
+    greedy = torch.tensor([t == 0.0 for t in T], device=DEV)
+    assert torch.equal(accepted[greedy], ga[greedy]) and torch.equal(emitted[greedy], ge[greedy])
+    for b in range(nB):
+        for j in range(int(accepted[b]) + 1):
+            assert p[b, j, emitted[b, j]] > -math.inf
+    assert len(set(accepted.tolist())) > 1

@@ -106,3 +106,22 @@ def test_the_reference_agrees_with_torch_about_e4m3(td):
     assert torch.equal(codes, torch.ldexp(x.float(), -e[:, None]).to(torch.float8_e4m3fn).view(torch.uint8))
     top = x.double().abs().amax(-1)
     assert (top <= 448 * 2.0 ** e).all() and (top > 224 * 2.0 ** e).all()
+
+
+def test_truncation_arguments(B):
+    def call(rules=True, logits=FAKE, dtype=B.DTYPE_F32, stride=1000, nB=2, s=3, V=1000, u=FAKE, out=FAKE + 64, tokens=FAKE):
+        return B.lib.spec_truncate_logits(None, logits, dtype, stride, nB, s, V, C.byref(B.SamplingRulesDesc()) if rules else None, u, None, 0, out, tokens)
+    for kw in (dict(nB=-1), dict(s=-1), dict(V=0), dict(dtype=7), dict(stride=999), dict(rules=False), dict(logits=None), dict(out=None, tokens=None),
+               dict(u=None), dict(logits=FAKE + 2), dict(out=FAKE + 2), dict(dtype=B.DTYPE_BF16, out=FAKE), dict(stride=1004, out=FAKE)):
+        assert call(**kw) == B.ERR_INVALID_ARG, kw
+        assert b"spec_truncate_logits" in B.lib.spec_last_error(None)
+    for kw in (dict(s=16), dict(nB=65536), dict(V=(1 << 28) + 1, stride=1 << 29)):
+        assert call(**kw) == B.ERR_CAPACITY, kw
+    assert call(nB=0, logits=None, out=None, tokens=None) == B.OK
+    n = C.c_size_t(1)
+    assert B.lib.spec_truncate_logits_workspace_bytes(1, 0, 32000, C.byref(n)) == B.OK
+    assert B.lib.spec_truncate_logits_workspace_bytes(1, 16, 32000, C.byref(n)) == B.ERR_CAPACITY
+    assert B.lib.spec_truncate_logits_workspace_bytes(1, 0, 0, C.byref(n)) == B.ERR_INVALID_ARG
+    assert B.lib.spec_truncate_logits_workspace_bytes(1, 0, 10, None) == B.ERR_INVALID_ARG
+    with pytest.raises(AssertionError):
+        B.SamplingRules(top_p=torch.ones(2))
