@@ -533,6 +533,10 @@ int spec_paged8_append(void *hip_stream, const spec_paged_cache8 *cache, const s
                        int64_t v_stride, void *d_q_out, int64_t q_out_stride);
 int spec_paged8_read(void *hip_stream, const spec_paged_cache8 *cache, const spec_paged_batch *batch, void *d_k, int64_t k_stride, void *d_v,
                      int64_t v_stride);
+int spec_paged8_attention_workspace_bytes(const spec_paged_cache8 *cache, const spec_paged_batch *batch, int32_t n_q_heads, size_t *bytes);
+int spec_paged8_attention(void *hip_stream, const spec_paged_cache8 *cache, const spec_paged_batch *batch, int32_t n_q_heads, const void *d_q,
+                          int64_t q_stride, float scale, int32_t window, void *d_workspace, size_t workspace_bytes, void *d_out,
+                          int64_t out_stride);
 
 /* Parity aids for the draft step (the call speculate(S, kv_SSM, s) of Alg. 1).
    spec_set_draft_logits: if d_logits is not NULL, every following spec_draft_step also writes the draft

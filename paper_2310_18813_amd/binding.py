@@ -33,7 +33,8 @@ EXPORTS = ["spec_last_error", "spec_workspace_bytes", "spec_init", "spec_destroy
            "spec_set_draft_logits", "spec_read_proposals", "spec_greedy_accept_workspace_bytes", "spec_greedy_accept",
            "spec_greedy_accept_noalloc", "spec_set_gemm_tuning", "spec_read_saturation", "spec_sample_tokens",
            "spec_sample_accept", "spec_set_sampling", "spec_paged_append", "spec_paged_attention_workspace_bytes",
-           "spec_paged_attention", "spec_paged_append_normed", "spec_paged8_append", "spec_paged8_read", "spec_process_logits", "spec_set_logit_rules",
+           "spec_paged_attention", "spec_paged_append_normed", "spec_paged8_append", "spec_paged8_read",
+           "spec_paged8_attention_workspace_bytes", "spec_paged8_attention", "spec_process_logits", "spec_set_logit_rules",
            "spec_truncate_logits_workspace_bytes", "spec_truncate_logits"]
 KCLASS_NAMES = ["gemm_qkv", "gemm_o", "gemm_ffn_in", "gemm_ffn_out", "gemm_head", "attention", "norm", "other",
                 "draft_pass"]
@@ -132,6 +133,9 @@ lib.spec_paged_append_normed.argtypes = [_vp, C.POINTER(PagedCacheDesc)] + _head
 lib.spec_paged8_append.argtypes = [_vp, C.POINTER(PagedCache8Desc)] + _heads_args
 lib.spec_paged8_read.argtypes = [_vp, C.POINTER(PagedCache8Desc), C.POINTER(PagedBatchDesc), _vp, _i64, _vp, _i64]
 lib.spec_process_logits.argtypes = [_vp, _vp, _i32, _i64, _i32, _i32, _i32, C.POINTER(LogitRulesDesc), _vp, _vp]
+lib.spec_paged8_attention_workspace_bytes.argtypes = [C.POINTER(PagedCache8Desc), C.POINTER(PagedBatchDesc), _i32, C.POINTER(C.c_size_t)]
+lib.spec_paged8_attention.argtypes = [_vp, C.POINTER(PagedCache8Desc), C.POINTER(PagedBatchDesc), _i32, _vp, _i64, C.c_float, _i32, _vp, C.c_size_t,
+                                      _vp, _i64]
 lib.spec_truncate_logits_workspace_bytes.argtypes = [_i32, _i32, _i32, C.POINTER(C.c_size_t)]
 lib.spec_truncate_logits.argtypes = [_vp, _vp, _i32, _i64, _i32, _i32, _i32, C.POINTER(SamplingRulesDesc), _vp, _vp, C.c_size_t, _vp, _vp]
 lib.spec_set_logit_rules.argtypes = [_vp, C.POINTER(LogitRulesDesc), _vp]
@@ -554,9 +558,7 @@ def spec_paged_attention_workspace_bytes(cache, batch, n_q_heads):
     return n.value
 
 
-def spec_paged_attention(cache, batch, q, scale=None, window=0, out=None, workspace=None):
-    """q [rows][n_q_heads][head_dim] over the pages -> out, the same shape.  scale: 1 / sqrt(head_dim) if None.  workspace: a uint8
-    tensor of spec_paged_attention_workspace_bytes() (allocated if None)."""
+def _attention(fn, workspace_bytes, cache, batch, q, scale, window, out, workspace):
     rows = batch.rows
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
@@ -564,11 +566,28 @@ def spec_paged_attention(cache, batch, q, scale=None, window=0, out=None, worksp
     op, os_, no = _heads(out, rows, cache)
     assert no == nq
     if workspace is None:
-        workspace = torch.empty(spec_paged_attention_workspace_bytes(cache, batch, nq), dtype=torch.uint8, device=q.device)
+        workspace = torch.empty(workspace_bytes(cache, batch, nq), dtype=torch.uint8, device=q.device)
     assert workspace.dtype is torch.uint8 and workspace.is_contiguous() and workspace.get_device() == batch.on
-    _call(cache.device, lib.spec_paged_attention, cache.ref, batch._for(cache), nq, qp, qs, cache.scale if scale is None else scale, window,
+    _call(cache.device, fn, cache.ref, batch._for(cache), nq, qp, qs, cache.scale if scale is None else scale, window,
           workspace.data_ptr() or None, workspace.numel(), op, os_)
     return out
+
+
+def spec_paged_attention(cache, batch, q, scale=None, window=0, out=None, workspace=None):
+    """q [rows][n_q_heads][head_dim] over the pages -> out, the same shape.  scale: 1 / sqrt(head_dim) if None.  workspace: a uint8
+    tensor of spec_paged_attention_workspace_bytes() (allocated if None)."""
+    return _attention(lib.spec_paged_attention, spec_paged_attention_workspace_bytes, cache, batch, q, scale, window, out, workspace)
+
+
+def spec_paged8_attention_workspace_bytes(cache, batch, n_q_heads):
+    n = C.c_size_t(0)
+    _check(lib.spec_paged8_attention_workspace_bytes(cache.ref, batch._for(cache), n_q_heads, C.byref(n)))
+    return n.value
+
+
+def spec_paged8_attention(cache, batch, q, scale=None, window=0, out=None, workspace=None):
+    """spec_paged_attention over a PagedCache8."""
+    return _attention(lib.spec_paged8_attention, spec_paged8_attention_workspace_bytes, cache, batch, q, scale, window, out, workspace)
 
 
 def spec_workspace_bytes(tgt_desc, drf_desc, run):

@@ -131,21 +131,26 @@ def attention(k, v, batch, q, scale, window):
     G = Hq // Hk
     out, err = torch.full(q.shape, math.nan, dtype=torch.float64), torch.zeros(q.shape, dtype=torch.float64)
     for b in range(batch.B):
-        for i in range(batch.rows[b]):
-            row, pos = batch.row_start[b] + i, batch.lens[b] - batch.rows[b] + i
-            lo = max(0, pos - window + 1) if window else 0
-            at = [(int(batch.table[b, p // batch.page]), p % batch.page) for p in range(lo, pos + 1)]
-            at = [(g, r) for g, r in at if 0 <= g < batch.n_pages]
-            if not at:
-                out[row] = 0.0
-                continue
-            pg, pr = (torch.tensor(x) for x in zip(*at))
-            K, V = k[pg, pr], v[pg, pr]
-            for h in range(Hq):
-                x, Kh, Vh = q[row, h].double(), K[:, h // G], V[:, h // G]
-                w = torch.softmax(Kh @ x * scale, 0)
-                out[row, h] = w @ Vh
-                size = w @ Vh.abs()
-                e = 2 * (hd + 8) * 2.0 ** -24 * float((Kh.abs() @ x.abs()).max()) * scale + (len(at) + 64) * 2.0 ** -24
-                err[row, h] = size * (e + u) * 1.01 + u * (out[row, h].abs() + u * size)
+        n, kv, r0 = batch.rows[b], batch.lens[b], batch.row_start[b]
+        if n == 0:
+            continue
+        out[r0:r0 + n] = 0.0
+        at = [(int(batch.table[b, p // batch.page]), p % batch.page, p) for p in range(kv)]
+        at = [x for x in at if 0 <= x[0] < batch.n_pages]
+        if not at:
+            continue
+        pg, pr, key = (torch.tensor(x) for x in zip(*at))
+        pos = torch.arange(kv - n, kv)[:, None]
+        see = (key <= pos) & ((key > pos - window) if window else torch.tensor(True))
+        K, V = k[pg, pr], v[pg, pr]  # [n][Hk][hd]
+        odd = ~torch.isfinite(V).all(-1)  # a position with a NaN among its values makes NaN of the rows that see it
+        for h in range(Hq):
+            x, Kh, Vh = q[r0:r0 + n, h].double(), K[:, h // G], torch.where(odd[:, h // G, None], 0.0, V[:, h // G])
+            z = torch.where(see, x @ Kh.t() * scale, -math.inf)
+            some = see.any(1)
+            w = torch.where(some[:, None], torch.softmax(torch.where(some[:, None], z, 0.0), 1), 0.0)
+            o, size = w @ Vh, w @ Vh.abs()
+            e = 2 * (hd + 8) * 2.0 ** -24 * torch.where(see, x.abs() @ torch.nan_to_num(Kh).abs().t(), 0.0).amax(1) * scale + (len(at) + 64) * 2.0 ** -24
+            err[r0:r0 + n, h] = size * (e[:, None] + u) * 1.01 + u * (o.abs() + u * size)
+            out[r0:r0 + n, h] = torch.where((see & odd[:, h // G]).any(1)[:, None], math.nan, o)
     return out, err

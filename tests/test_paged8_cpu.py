@@ -125,3 +125,27 @@ def test_truncation_arguments(B):
     assert B.lib.spec_truncate_logits_workspace_bytes(1, 0, 10, None) == B.ERR_INVALID_ARG
     with pytest.raises(AssertionError):
         B.SamplingRules(top_p=torch.ones(2))
+
+
+def test_attention_over_8_bits_arguments(B):
+    def attend(c, b, **kw):
+        a = dict(nq=4, q=FAKE, qs=512, scale=0.1, window=0, ws=None, wb=0, out=FAKE, outs=512)
+        a.update(kw)
+        return B.lib.spec_paged8_attention(None, C.byref(c) if c else None, C.byref(b) if b else None, *a.values())
+    for kw, code in BAD_CACHE8:
+        assert attend(cache8(B, **kw), batch(B)) == getattr(B, "ERR_" + code), kw
+        assert b"spec_paged8_attention" in B.lib.spec_last_error(None)
+    for kw, code in BAD_BATCH:
+        assert attend(cache8(B), batch(B, **kw)) == getattr(B, "ERR_" + code), kw
+    assert attend(None, batch(B)) == attend(cache8(B), None) == B.ERR_INVALID_ARG
+    for kw in (dict(nq=0), dict(nq=3), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")), dict(scale=float("nan")), dict(scale=2.4e38), dict(window=-1),
+               dict(q=None), dict(q=FAKE + 8), dict(qs=500), dict(out=None), dict(outs=256)):
+        assert attend(cache8(B), batch(B), **kw) == B.ERR_INVALID_ARG, kw
+    long, n = batch(B, pages_stride=1000, max_len=16000), C.c_size_t(0)
+    assert B.lib.spec_paged8_attention_workspace_bytes(C.byref(cache8(B)), C.byref(long), 4, C.byref(n)) == B.OK and n.value > 0
+    for kw in (dict(), dict(ws=FAKE + 16, wb=n.value), dict(ws=FAKE, wb=n.value - 1)):
+        assert attend(cache8(B), long, **kw) == B.ERR_WORKSPACE
+    assert attend(cache8(B), batch(B, rows=1 << 29, max_rows=1 << 29, d_row_start=FAKE)) == B.ERR_CAPACITY
+    assert attend(cache8(B), batch(B, B=0, rows=0)) == B.OK and attend(cache8(B), batch(B, rows=0)) == B.OK
+    assert B.lib.spec_paged8_attention_workspace_bytes(C.byref(cache8(B, dtype=0)), C.byref(long), 4, C.byref(n)) == B.ERR_UNSUPPORTED
+    assert B.lib.spec_paged8_attention_workspace_bytes(C.byref(cache8(B)), C.byref(long), 4, None) == B.ERR_INVALID_ARG
