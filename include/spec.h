@@ -403,7 +403,7 @@ typedef struct {
      is fp32 and row_stride = vocab.
      d_tokens [B][s+1] or NULL (not both): a draw from the kept tokens with d_uniforms [B][s+1], numbers in [0, 1): the lowest id whose cumulative weight
      exceeds u times the sum.  A row without any token above -infinity yields -infinity throughout and token 0.
-     d_workspace: scratch of spec_truncate_logits_workspace_bytes() (which may be 0: then NULL), 256-byte aligned; calls that may overlap need one each.
+     d_workspace: scratch of spec_truncate_logits_workspace_bytes(), 256-byte aligned; calls that may overlap need one each.
    Weights are whole multiples of 2^-50 (2^(bits - 62) with vocabularies of more than 2^12 tokens, of up to 2^bits) and computed in 64 bits, so
    their sums are exact and the same in whatever order: which tokens are kept and drawn differs from the definition only where a sum comes within
    some 10^-12 of its limit.  Enqueues on hip_stream (NULL = the default stream), needs no context, does not wait.

@@ -7,8 +7,15 @@
 // was taken in.  So weights are whole numbers, e^x times a power of two to nearest, and sums of them are exact: 2^50 for
 // a weight of 1 up to 4096 tokens, 2^44 with 151936.  Their exponential is computed in 64 bits (a power of two times a polynomial of degree 10 on half an octave).
 //
-// A workgroup takes a row.  Passes: the largest logit; counts and sums of weights by bins of 1/64 octave of the weight, in LDS; the tokens of
-// the bin with the border, listed in LDS and narrowed down; the result.  Only where a bin has more tokens than the list does narrowing go over the row.
+// Rows differ in what they ask for, and a row has more work than a compute unit does quickly, so that all but the search for the border
+// is cut into pieces of rows:
+//   k_row_maxima    the largest logit of every 16 tokens, and of every piece
+//   k_row_masses    (rows with top-p over all tokens, or a large top-k) counts and sums of weights by bins of 1/64 octave of the weight
+//   k_row_border    a workgroup a row: what may hold the border, listed in LDS and narrowed down 8 bits of its places at a time.  For a small top-k
+//                   that are the tokens above the k-th largest of the 16s' maxima, else those up to the bin in which the count or the sum reaches
+//                   its limit.  What the maxima rule out is not read.  Draws, where all that is kept is in the list.
+//   k_row_finish    the result; logits that the maxima rule out are not read.  Sums of the kept weights by 256 tokens, for
+//   k_row_draw      the other rows' draws.
 #include "spec_internal.h"
 #include "device_utils.h"
 #include <algorithm>
@@ -18,37 +25,57 @@ namespace spec {
 
 typedef unsigned long long u64;
 
-constexpr int TR_BINS = 2048, TR_LIST = 4096, TR_FINE = 256, TR_SEGS = 256;
+constexpr int TR_BINS = 2048, TR_PER_OCTAVE = 64;  // bins of weights: 32 octaves of them
+constexpr int TR_FINE = 256;   // parts that what is looked at is cut into
+constexpr int TR_LAST = 128;   // tokens that are put in order at once
+constexpr int TR_FEW = 1024;   // the largest top-k that goes by the maxima alone
+constexpr int TR_PIECES = 64;  // of a row, for its maxima
+
+// What is found out about a row: kept is a logit that is larger than last_z, or equal with an id up to last_id; x = (z - zero) / temp.
+struct RowBorder {
+  double c;  // log2(e) / temp
+  float last_z, zero, temp;
+  int last_id;
+  int endless, drawn;
+};
 
 struct TruncateArgs {
   const void *logits;
   int64_t row_stride;
-  int q, V, shift;  // rows of a sequence; a weight of 1 is 2^shift
+  int row0, q, V, shift;  // first row of the launch; rows of a sequence; a weight of 1 is 2^shift
   const float *temperature;
   const int32_t *top_k;
   const float *top_p, *min_p;
   float *out;
   const float *u;
   int32_t *tokens;
+  // workspace
+  float *piece_max, *max16;   // [rows][TR_PIECES], [rows][n16]
+  RowBorder *border;          // [rows]
+  u64 *sums, *masses;         // [rows][stretches], [rows][cuts][TR_BINS]
+  uint32_t *counts;           // [rows][cuts][TR_BINS]
+  int pieces, piece;          // pieces of a row and tokens of one (a multiple of 1024), for the maxima
+  int cuts, cut, B;           // for the masses; sequences
+  int n16, stretches;         // 16s and 256s of a row
 };
 
-// Four logits from token x on (a multiple of four); NaN and what lies behind the row are -infinity.
-template <class T, bool VEC>
-__device__ __forceinline__ void row4(const T *row, int x, int V, float (&z)[4]) {
-  if constexpr (VEC) {
-    T v[4];
-    const int at = min(x, V - 4);
-    __builtin_memcpy(v, __builtin_assume_aligned(row + at, 4 * sizeof(T)), 4 * sizeof(T));
+// Four logits from token x on (a multiple of four) as they lie in memory, from within the row wherever x is.
+template <class T, bool VEC> struct Quad {
+  T v[4];
+  __device__ __forceinline__ void load(const T *row, int x, int V) {
+    if constexpr (VEC) {
+      __builtin_memcpy(v, __builtin_assume_aligned(row + min(x, V - 4), 4 * sizeof(T)), 4 * sizeof(T));
+    } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) z[i] = x < V ? fmaxf(Conv<T>::ld(v, i), -INFINITY) : -INFINITY;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float v = Conv<T>::ld(row, min(x + i, V - 1));
-      z[i] = x + i < V ? fmaxf(v, -INFINITY) : -INFINITY;
+      for (int i = 0; i < 4; ++i) v[i] = row[min(x + i, V - 1)];
     }
   }
-}
+  // NaN and what lies behind the row are -infinity
+  __device__ __forceinline__ void numbers(int x, int V, float (&z)[4]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) z[i] = (VEC ? x : x + i) < V ? fmaxf(Conv<T>::ld(v, i), -INFINITY) : -INFINITY;
+  }
+};
 
 // A token's place in the order.  (-0 and 0 are the same logit.)
 __device__ __forceinline__ u64 place_of(float z, int id) {
@@ -61,14 +88,13 @@ __device__ __forceinline__ float logit_of(u64 place) {
   return __uint_as_float(up & 0x80000000u ? up & 0x7fffffffu : ~up);
 }
 
-// A row's weights: log2 of one, its bin, and itself as a whole number.
+// A row's weights: log2 of one, and itself as a whole number.
 struct Weights {
   double M, c;  // largest logit, log2(e) / temperature
   int shift;
   __device__ __forceinline__ double log2_of(float z) const { return fmax(((double)z - M) * c, -1100.); }  // (-infinity at any temperature as well)
-  __device__ __forceinline__ int bin(double y) const { return min(TR_BINS - 1, (int)(y * -64.)); }
-  __device__ __forceinline__ u64 number(double y) const {
-    const double n = rint(y), f = y - n;
+  __device__ __forceinline__ u64 number(float z) const {
+    const double y = log2_of(z), n = rint(y), f = y - n;
     // the Taylor series of 2^f: what is left out is below (ln 2 / 2)^11 / 11! = 2.2e-13 of it
     double p = 7.0549116208011233e-9;
     p = fma(p, f, 1.0178086009239699e-7);
@@ -86,27 +112,74 @@ struct Weights {
   }
 };
 
-template <int NT> struct TruncateShared {
-  u64 list[TR_LIST], mass[TR_BINS], fine_mass[TR_FINE], seg[TR_SEGS], wave_u[2][NT / 64], found_mass, found_place;
-  uint32_t cnt[TR_BINS], fine_cnt[TR_FINE], wave_c[NT / 64], found_bin, found_cnt, found_n, listed;
+// What a row asks for, and what its weights are.
+struct RowRules {
+  float temp, p, floor_p;
+  int k;
+  bool by_k, by_p, few, dense;  // few: the border of top-k goes by the maxima; dense: bins are needed
+  __device__ __forceinline__ RowRules(const TruncateArgs &a, int b) {
+    temp = a.temperature ? a.temperature[b] : 1.f;
+    const bool greedy = !(temp > 0.f);
+    k = greedy ? 1 : a.top_k ? a.top_k[b] : 0;
+    p = greedy || !a.top_p ? 1.f : a.top_p[b];
+    floor_p = greedy || !a.min_p ? 0.f : a.min_p[b];
+    if (greedy) temp = 1.f;
+    by_k = k > 0 && k < a.V;
+    by_p = p < 1.f && k != 1;
+    few = by_k && k <= min(TR_FEW, a.n16 / 2);
+    dense = k != 1 && !few && (by_k || by_p);
+  }
+};
+struct RowScale {
+  float top, zero;  // the largest logit; 0 where it is infinite: then infinite ones share the weight and the others have none, and 0 and -infinity stand for them
+  bool endless;
+  Weights wt;
+  float per_unit;
+  __device__ __forceinline__ RowScale(const TruncateArgs &a, int row, float temp) {
+    const int lane = threadIdx.x & 63;
+    top = wave_max(a.piece_max[(int64_t)row * TR_PIECES + min(lane, a.pieces - 1)]);
+    endless = top == INFINITY;
+    zero = endless ? 0.f : top;
+    wt = Weights{(double)zero, 1.4426950408889634074 / (double)temp, a.shift};
+    per_unit = fminf((float)(wt.c * TR_PER_OCTAVE), 3e38f);
+  }
+  __device__ __forceinline__ float of(float z) const { return !endless ? z : z == INFINITY ? 0.f : -INFINITY; }
+  // A token's bin, which never falls as its logit falls.  (0 times infinity would be the last one's.)
+  __device__ __forceinline__ int bin(float z) const { return (int)fminf((zero - z) * per_unit, (float)(TR_BINS - 1)); }
 };
 
-__device__ __forceinline__ u64 wave_sum(u64 v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, 64);
+// What a workgroup of NT threads that looks for a border holds.
+template <int NT> struct Truncate {
+  static constexpr int WAVES = NT / 64, LIST = NT == 256 ? 1024 : 4096;
+  u64 list[LIST], mass[TR_BINS], fine_mass[TR_FINE], last_mass[TR_LAST], wave_u[2][WAVES], found_mass, found_place;
+  uint32_t cnt[TR_BINS], fine_cnt[TR_FINE], wave_c[WAVES], found_bin, found_cnt, found_n, listed, few;
+  static constexpr int UNITS = TR_BINS / 2;  // sums of weights over stretches of the row, in the place of mass
+};
+
+// Sums and maxima over the lanes of a wave up to each lane (so that the last one has that of all), without a trip through LDS.
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t shifted(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+template <int CTRL, int ROWS> __device__ __forceinline__ u64 shifted(u64 v) {
+  return (u64)shifted<CTRL, ROWS>((uint32_t)(v >> 32)) << 32 | shifted<CTRL, ROWS>((uint32_t)v);
+}
+template <class V> __device__ __forceinline__ V sum_to_lane(V v) {
+  v += shifted<0x111, 0xf>(v); v += shifted<0x112, 0xf>(v); v += shifted<0x114, 0xf>(v); v += shifted<0x118, 0xf>(v);
+  v += shifted<0x142, 0xa>(v); v += shifted<0x143, 0xc>(v);
+  return v;
+}
+__device__ __forceinline__ u64 max_to_lane(u64 v) {
+  v = max(v, shifted<0x111, 0xf>(v)); v = max(v, shifted<0x112, 0xf>(v)); v = max(v, shifted<0x114, 0xf>(v)); v = max(v, shifted<0x118, 0xf>(v));
+  v = max(v, shifted<0x142, 0xa>(v)); v = max(v, shifted<0x143, 0xc>(v));
   return v;
 }
 
-// The sums of counts and weights up to a thread's own, and of all.  (Reads back sh.wave_*: two barriers.)
-template <int NT>
-__device__ __forceinline__ void scan(TruncateShared<NT> &sh, uint32_t &c, u64 &m, uint32_t &all_c, u64 &all_m) {
+// The sums of counts and weights up to a thread's own, and of all.
+template <int NT, class Sh>
+__device__ __forceinline__ void scan(Sh &sh, uint32_t &c, u64 &m, uint32_t &all_c, u64 &all_m) {
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t uc = __shfl_up(c, o, 64);
-    const u64 um = __shfl_up(m, o, 64);
-    if (lane >= o) { c += uc; m += um; }
-  }
+  c = sum_to_lane(c);
+  m = sum_to_lane(m);
   __syncthreads();
   if (lane == 63) { sh.wave_c[wv] = c; sh.wave_u[0][wv] = m; }
   __syncthreads();
@@ -121,9 +194,9 @@ __device__ __forceinline__ void scan(TruncateShared<NT> &sh, uint32_t &c, u64 &m
 // Among N bins of counts and sums, the one in which `target` is reached, by sum or by count; what lies before it goes on top of what
 // is there in before_*.  Leaves the bin and its count; false if no bin reaches it.
 template <int NT, int N>
-__device__ __forceinline__ bool find_bin(TruncateShared<NT> &sh, const uint32_t *cnt, const u64 *mass, bool by_mass, u64 target, uint32_t &before_cnt,
+__device__ __forceinline__ bool find_bin(Truncate<NT> &sh, const uint32_t *cnt, const u64 *mass, bool by_mass, u64 target, uint32_t &before_cnt,
                                          u64 &before_mass, int &bin, uint32_t &n) {
-  constexpr int PER = N / NT > 0 ? N / NT : 1;
+  constexpr int PER = (N + NT - 1) / NT;
   const int first = threadIdx.x * PER;
   uint32_t c[PER];
   u64 m[PER];
@@ -137,6 +210,7 @@ __device__ __forceinline__ bool find_bin(TruncateShared<NT> &sh, const uint32_t 
   }
   uint32_t to_c = sc, all_c;
   u64 to_m = sm, all_m;
+  __syncthreads();
   if (threadIdx.x == 0) sh.found_bin = ~0u;
   scan<NT>(sh, to_c, to_m, all_c, all_m);
   to_c += before_cnt - sc; to_m += before_mass - sm;
@@ -155,266 +229,622 @@ __device__ __forceinline__ bool find_bin(TruncateShared<NT> &sh, const uint32_t 
   return true;
 }
 
-template <class T, bool VEC, int NT>
-__global__ __launch_bounds__(NT) void k_truncate_logits(TruncateArgs a) {
-  __shared__ TruncateShared<NT> sh;
-  const int row = blockIdx.x, b = row / a.q, lane = threadIdx.x & 63, wv = threadIdx.x >> 6, V = a.V;
-  const T *z_row = (const T *)a.logits + (int64_t)row * a.row_stride;
-  float *out = a.out ? a.out + (int64_t)row * V : nullptr;
-  float temp = a.temperature ? a.temperature[b] : 1.f;
-  const bool greedy = !(temp > 0.f);
-  int k = greedy ? 1 : a.top_k ? a.top_k[b] : 0;
-  const float p = greedy || !a.top_p ? 1.f : a.top_p[b];
-  float floor_p = greedy || !a.min_p ? 0.f : a.min_p[b];
-  if (greedy) temp = 1.f;
+template <int CTRL> __device__ __forceinline__ float from_lane(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
 
-  // the largest logit and its lowest token
-  u64 best = ~0ull;
-  for (int x = 4 * threadIdx.x; x < V; x += 4 * NT) {
-    float z[4];
-    row4<T, VEC>(z_row, x, V, z);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) best = min(best, place_of(z[i], x + i));
+struct Kept {
+  float last_z;
+  int last_id;
+  __device__ __forceinline__ bool operator()(float z, int id) const { return z > last_z || (z == last_z && id <= last_id); }
+};
+
+// What a draw needs of LDS (a workgroup that looked for a border has it).
+template <int NT> struct DrawShared {
+  u64 wave_u[2][NT / 64], found_mass;
+  uint32_t wave_c[NT / 64], found_bin;
+};
+
+// The draw of a row: the first token with which the sum of the kept weights, in the order of ids, exceeds u times their total.  sums: of n stretches of
+// per * 256 tokens.
+template <class T, bool VEC, int NT, class Sh>
+__device__ __forceinline__ void draw_token(Sh &sh, const TruncateArgs &a, int row, const RowScale &sc, const Kept &kept, const u64 *sums, int n, int per) {
+  const int lane = threadIdx.x & 63, each = (n + NT - 1) / NT, s0 = min(n, (int)threadIdx.x * each), s1 = min(n, s0 + each);
+  const T *z_row = (const T *)a.logits + (int64_t)row * a.row_stride;
+  u64 own = 0, total;
+  for (int s = s0; s < s1; ++s) own += sums[s];
+  if (threadIdx.x == 0) { sh.found_bin = 0; sh.found_mass = 0; }
+  u64 to = own;
+  uint32_t none = 0, no_c;
+  scan<NT>(sh, none, to, no_c, total);
+  const double want = (double)a.u[row] * (double)total;
+  const u64 target = want > 0. ? min(total - 1, (u64)want) : 0;  // exceeded from target + 1 on
+  u64 at = to - own;
+  if (at <= target && to > target) {
+    for (int s = s0; s < s1; ++s) {
+      const u64 next = at + sums[s];
+      if (next > target) { sh.found_bin = s; sh.found_mass = at; break; }
+      at = next;
+    }
   }
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) best = min(best, (u64)__shfl_xor(best, o, 64));
-  if (lane == 0) sh.wave_u[0][wv] = best;
-  for (int i = threadIdx.x; i < TR_BINS; i += NT) { sh.mass[i] = 0; sh.cnt[i] = 0; }
-  for (int i = threadIdx.x; i < TR_SEGS; i += NT) sh.seg[i] = 0;
   __syncthreads();
+  if (threadIdx.x >= 64) return;
+  u64 before = sh.found_mass;
+  for (int s = (int)sh.found_bin * per; s < min(a.stretches, ((int)sh.found_bin + 1) * per) && before <= target; ++s) {
+    const int x = 256 * s + 4 * lane;
+    Quad<T, VEC> v;
+    float z[4];
+    v.load(z_row, x, a.V);
+    v.numbers(x, a.V, z);
+    u64 w[4], sum = 0;
 #pragma unroll
-  for (int i = 0; i < NT / 64; ++i) best = min(best, sh.wave_u[0][i]);
-  const float top = logit_of(best);
-  if (top == -INFINITY) {
-    if (out)
-      for (int x = threadIdx.x; x < V; x += NT) out[x] = -INFINITY;
-    if (threadIdx.x == 0 && a.tokens) a.tokens[row] = 0;
+    for (int i = 0; i < 4; ++i) {
+      z[i] = sc.of(z[i]);
+      w[i] = kept(z[i], x + i) ? sc.wt.number(z[i]) : 0;
+      sum += w[i];
+    }
+    const u64 up_to = sum_to_lane(sum);
+    u64 c = before + up_to - sum;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (c <= target && c + w[i] > target) a.tokens[row] = x + i;
+      c += w[i];
+    }
+    before += __shfl(up_to, 63, 64);
+  }
+}
+
+// ------------------------------------------------------------------ pieces of rows
+template <class T, bool VEC>
+__global__ __launch_bounds__(256) void k_row_maxima(TruncateArgs a) {
+  __shared__ float sh[4];
+  const int row = a.row0 + blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces, V = a.V;
+  const T *z_row = (const T *)a.logits + (int64_t)row * a.row_stride;
+  float *max16 = a.max16 + (int64_t)row * a.n16;
+  float top = -INFINITY;
+  for (int x0 = piece * a.piece + 4 * threadIdx.x; x0 - 4 * (int)(threadIdx.x & 63) < min(V, (piece + 1) * a.piece); x0 += 4096) {  // (whole waves)
+    Quad<T, VEC> v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i].load(z_row, x0 + 1024 * i, V);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int x = x0 + 1024 * i;
+      float z[4];
+      v[i].numbers(x, V, z);
+      float t = fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3]));
+      t = fmaxf(t, from_lane<0xb1>(t));
+      t = fmaxf(t, from_lane<0x4e>(t));
+      top = fmaxf(top, t);
+      if ((threadIdx.x & 3) == 0 && x < V) max16[x >> 4] = t;
+    }
+  }
+  top = wave_max(top);
+  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = top;
+  __syncthreads();
+  if (threadIdx.x == 0) a.piece_max[(int64_t)row * TR_PIECES + piece] = fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
+}
+
+// Which rows need bins is on the device.  With up to 64 sequences these rows share the pieces that there is room for, with more a row has its own.
+struct Cuts {
+  u64 dense;      // sequences that need bins
+  int each, cut;  // pieces of a row, tokens of one
+  __device__ __forceinline__ Cuts(const TruncateArgs &a) {
+    dense = 0;
+    each = a.cuts;
+    if (a.B <= 64) {
+      const int lane = threadIdx.x & 63;
+      dense = __ballot(lane < a.B && RowRules(a, min(lane, a.B - 1)).dense);
+      each = max(each, min((a.V + 4095) / 4096, a.B * a.cuts / max(1, __popcll(dense))));
+    }
+    cut = ((a.V + each * 4096 - 1) / (each * 4096)) * 4096;
+    each = (a.V + cut - 1) / cut;
+  }
+  // the first piece of a row
+  __device__ __forceinline__ int64_t first(const TruncateArgs &a, int row) const {
+    if (a.B > 64) return (int64_t)row * a.cuts;
+    return (int64_t)(__popcll(dense & ((1ull << (row / a.q)) - 1)) * a.q + row % a.q) * each;
+  }
+};
+
+template <class T, bool VEC>
+__global__ __launch_bounds__(512) void k_row_masses(TruncateArgs a) {
+  __shared__ u64 mass[TR_BINS];
+  __shared__ uint32_t cnt[TR_BINS];
+  const Cuts cuts(a);
+  int row = a.row0 + blockIdx.x / cuts.each;
+  const int cut = blockIdx.x % cuts.each, V = a.V;
+  if (a.B <= 64) {  // (all rows are one launch's then)
+    u64 left = cuts.dense;
+    const int nth = row / a.q;
+    if (nth >= __popcll(left)) return;
+    for (int i = 0; i < nth; ++i) left &= left - 1;
+    row = (__ffsll(left) - 1) * a.q + row % a.q;
+  }
+  const RowRules r(a, row / a.q);
+  if (!r.dense) return;
+  const RowScale sc(a, row, r.temp);
+  if (sc.top == -INFINITY) return;
+  const T *z_row = (const T *)a.logits + (int64_t)row * a.row_stride;
+  for (int i = threadIdx.x; i < TR_BINS; i += 512) { mass[i] = 0; cnt[i] = 0; }
+  __syncthreads();
+  const int end = min(V, (cut + 1) * cuts.cut);
+  for (int x0 = cut * cuts.cut + 4 * threadIdx.x; x0 < end; x0 += 8192) {
+    Quad<T, VEC> v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i].load(z_row, x0 + 2048 * i, V);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float z[4];
+      v[i].numbers(x0 + 2048 * i, end, z);
+      u64 w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = sc.wt.number(z[e] = sc.of(z[e]));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int at = sc.bin(z[e]);
+        if (z[e] > -INFINITY) {
+          atomicAdd(&mass[at], w[e]);
+          if (r.by_k) atomicAdd(&cnt[at], 1u);
+        }
+      }
+    }
+  }
+  __syncthreads();
+  const int64_t at = (cuts.first(a, row) + cut) * TR_BINS;
+  for (int i = threadIdx.x; i < TR_BINS; i += 512) {
+    a.masses[at + i] = mass[i];
+    if (r.by_k) a.counts[at + i] = cnt[i];
+  }
+}
+
+// ------------------------------------------------------------------ the border
+template <class T, bool VEC, int NT>
+__global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
+  typedef Truncate<NT> Sh;
+  __shared__ Sh sh;
+  const int row = a.row0 + blockIdx.x, lane = threadIdx.x & 63, wv = threadIdx.x >> 6, V = a.V;
+  const T *z_row = (const T *)a.logits + (int64_t)row * a.row_stride;
+  const float *max16 = a.max16 + (int64_t)row * a.n16;
+  const RowRules r(a, row / a.q);
+  const RowScale sc(a, row, r.temp);
+  const Weights &wt = sc.wt;
+  const int k = r.k;
+  if (sc.top == -INFINITY) {
+    if (threadIdx.x == 0) {
+      a.border[row] = RowBorder{wt.c, INFINITY, 0.f, 1.f, -1, 0, 1};  // (INFINITY: of numbers that are not larger, none is kept)
+      if (a.tokens) a.tokens[row] = 0;
+    }
     return;
   }
-  // Where the largest is infinite, infinite ones share the weight and the others have none: 0 and -infinity instead of them.
-  const bool endless = top == INFINITY;
-  const Weights wt{endless ? 0. : (double)top, 1.4426950408889634074 / (double)temp, a.shift};
-  auto fetch = [&](int x, float (&z)[4]) {
-    row4<T, VEC>(z_row, x, V, z);
-    if (endless) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) z[i] = z[i] == INFINITY ? 0.f : -INFINITY;
-    }
-  };
 
   // the border: the place of the last token that top-k and top-p keep
   u64 border = ~0ull;
+  bool from_list = false, all_listed = false;  // all_listed: the list has all that lies before the border as well
   if (k == 1) {
-    border = endless ? place_of(0.f, (int)(uint32_t)best) : best;
-  } else if ((k > 0 && k < V) || p < 1.f) {
-    for (int x = 4 * threadIdx.x; x < V; x += 4 * NT) {
-      float z[4];
-      fetch(x, z);
+    // the lowest token of the largest logit, in the first 16 that have it
+    if (threadIdx.x == 0) sh.few = ~0u;
+    __syncthreads();
+    uint32_t first = ~0u;
+    for (int g = threadIdx.x; g < a.n16; g += 8 * NT) {
+      float z[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (z[i] == -INFINITY) continue;
-        const double y = wt.log2_of(z[i]);
-        const int bin = wt.bin(y);
-        atomicAdd(&sh.cnt[bin], 1u);
-        atomicAdd(&sh.mass[bin], wt.number(y));
-      }
+      for (int i = 0; i < 8; ++i) z[i] = max16[min(g + i * NT, a.n16 - 1)];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (z[i] == sc.top) first = min(first, (uint32_t)min(g + i * NT, a.n16 - 1));
+    }
+    if (first != ~0u) atomicMin(&sh.few, first);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      int id = 16 * (int)sh.few;
+      while (id < min(V, 16 * (int)sh.few + 15) && !(Conv<T>::ld(z_row, id) == sc.top)) ++id;
+      sh.list[0] = place_of(sc.zero, id);
+      sh.listed = 1;
     }
     __syncthreads();
-    uint32_t all_c = 0;
-    u64 all_m = 0;
-    {
+    border = sh.list[0];
+    from_list = all_listed = true;
+  } else if (r.by_k || r.by_p) {
+    // What is looked at: the tokens of bins first .. last whose places lie in lo .. hi, n of them, of the row or of the list.  The border is the first of
+    // them with which the count, or by_mass the sum, on top of bc or bm, reaches `target`.
+    int first = 0, last = TR_BINS - 1;
+    u64 lo = 0, hi = ~0ull, bm = 0, all_m = 0, target = (u64)max(k, 1);
+    uint32_t n = 0, bc = 0, all_c = 0;
+    bool by_mass = false, searching = true;
+    auto part_of = [&](u64 total) { return max((u64)1, min(total, (u64)ceil(fmax((double)r.p, 0.) * (double)total))); };
+    // The bin where the count or the sum reaches `target` is looked at; with those before it where there is room for all.
+    auto look_at_bin = [&]() {
+      bc = 0; bm = 0; lo = 0; hi = ~0ull;
+      from_list = false;
+      const bool there = find_bin<NT, TR_BINS>(sh, sh.cnt, sh.mass, by_mass, target, bc, bm, last, n);
+      if (bc + n <= Sh::LIST) {
+        first = 0; n += bc; bc = 0; bm = 0;
+      } else {
+        first = last;
+      }
+      return there;
+    };
+    if (r.few) {
+      // The k-th largest of the 16s' maxima is no larger than the k-th of all, so that the tokens that are not in a bin behind its own, little
+      // more than k, have the first k among them.  (Of fewer than k finite ones all are kept.)
+      for (int i = threadIdx.x; i < TR_BINS; i += NT) { sh.cnt[i] = 0; sh.mass[i] = 0; }
+      __syncthreads();
+      for (int g = threadIdx.x; g < a.n16; g += 8 * NT) {
+        float z[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = max16[min(g + i * NT, a.n16 - 1)];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float y = sc.of(z[i]);
+          if (g + i * NT < a.n16 && y > -INFINITY) atomicAdd(&sh.cnt[sc.bin(y)], 1u);
+        }
+      }
+      __syncthreads();
+      if (!find_bin<NT, TR_BINS>(sh, sh.cnt, sh.mass, false, target, bc, bm, last, n)) last = TR_BINS - 1;
+      bc = 0; bm = 0; n = 0;
+    } else {
       uint32_t c = 0;
       u64 m = 0;
-      for (int i = threadIdx.x; i < TR_BINS; i += NT) { c += sh.cnt[i]; m += sh.mass[i]; }
-      scan<NT>(sh, c, m, all_c, all_m);
-    }
-
-    // The first token, among those of bin `of`, with which count or sum reaches `target` -> its place; before_*: in front of the bin, then up to
-    // and with the token.
-    auto resolve = [&](int of, uint32_t n, bool by_mass, u64 target, uint32_t &before_cnt, u64 &before_mass) {
-      u64 lo = 0, hi = ~0ull;
-      bool listed = false;
-      auto each = [&](auto f) {
-        if (listed) {
-          for (uint32_t i = threadIdx.x; i < min(sh.listed, (uint32_t)TR_LIST); i += NT) {
-            const u64 at = sh.list[i];
-            if (at >= lo && at <= hi) f(at);
-          }
-        } else {
-          for (int x = 4 * threadIdx.x; x < V; x += 4 * NT) {
-            float z[4];
-            fetch(x, z);
+      constexpr int PER = (TR_BINS + NT - 1) / NT;
+      const Cuts cuts(a);
+      const int64_t at = cuts.first(a, row) * TR_BINS + threadIdx.x;
+      u64 masses[PER] = {};
+      uint32_t counts[PER] = {};
+#pragma unroll 4
+      for (int cut = 0; cut < cuts.each; ++cut)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              if (z[i] == -INFINITY || wt.bin(wt.log2_of(z[i])) != of) continue;
-              const u64 at = place_of(z[i], x + i);
-              if (at >= lo && at <= hi) f(at);
-            }
+        for (int i = 0; i < PER; ++i) masses[i] += a.masses[at + cut * TR_BINS + min(i * NT, TR_BINS - 1 - (int)threadIdx.x)];
+      if (r.by_k)
+        for (int cut = 0; cut < cuts.each; ++cut)
+#pragma unroll
+          for (int i = 0; i < PER; ++i) counts[i] += a.counts[at + cut * TR_BINS + min(i * NT, TR_BINS - 1 - (int)threadIdx.x)];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int of = threadIdx.x + i * NT;
+        if (of >= TR_BINS) break;
+        // A bin's weights are alike, so that its sum tells how many there are, a little high (the last one's, which may be small, aside).
+        if (!r.by_k) counts[i] = masses[i] ? 1 + (uint32_t)(ldexpf((float)masses[i], -a.shift) * exp2f((of + 1) * (1.01f / TR_PER_OCTAVE))) : 0;
+        sh.mass[of] = masses[i]; sh.cnt[of] = counts[i];
+        c += counts[i]; m += masses[i];
+      }
+      scan<NT>(sh, c, m, all_c, all_m);
+      by_mass = !(r.by_k && (uint32_t)k < all_c);
+      if (by_mass) target = part_of(all_m);
+      searching = (r.by_p || !by_mass) && look_at_bin();
+    }
+    // One pass over what is looked at a turn, until it is few tokens: list it where there is room; else its bounds, and which of 256 parts between
+    // them has the border.  (Eight bits of at most 64 every two turns, for two borders: the limit is never met.)
+    enum { LIST, BOUNDS, PARTS, SUM, LAST };
+    bool bounded = true, summing = false;
+    int drop = 0;
+    u64 base = place_of(sc.zero, 0);
+    // Parts from the first bin on: they need not end where the bins do.
+    auto parts_to = [&](u64 end) {
+      drop = max(0, 64 - __clzll(end - base) - 8);
+      bounded = true;
+    };
+    auto parts_of_bins = [&]() {
+      base = place_of(first == 0 ? sc.zero : sc.zero - (float)(first - 1) / sc.per_unit, 0);
+      parts_to(max(base + 1, place_of(sc.zero - (float)(last + 2) / sc.per_unit, 0)));
+    };
+    parts_of_bins();
+#pragma unroll 1
+    for (int turn = 0; searching && turn < 48; ++turn) {
+      const int mode = summing ? SUM : !from_list && n <= Sh::LIST ? LIST : from_list && n <= TR_LAST ? LAST : bounded ? PARTS : BOUNDS;
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        if (mode == LIST) sh.listed = 0;
+        sh.few = 0;
+      }
+      if (mode == PARTS)
+        for (int i = threadIdx.x; i < TR_FINE; i += NT) { sh.fine_mass[i] = 0; sh.fine_cnt[i] = 0; }
+      __syncthreads();
+      u64 least = ~0ull, most = 0, sum = 0;
+      auto take = [&](u64 at, float z) {  // (lists and orders are below: a wave counts its tokens first, since a thousand additions to one word of LDS take 10 us)
+        if (at < lo || at > hi) return;
+        if (mode == BOUNDS) {
+          least = min(least, at); most = max(most, at);
+        } else {
+          const u64 w = wt.number(z);
+          sum += w;
+          if (mode == PARTS) {
+            const int part = (int)min((u64)(TR_FINE - 1), (at - min(at, base)) >> drop);
+            atomicAdd(&sh.fine_cnt[part], 1u);
+            atomicAdd(&sh.fine_mass[part], w);
           }
         }
       };
-      // (every turn takes 8 of at most 64 bits)
-      for (int turn = 0; turn < 10; ++turn) {
-        if (!listed && n <= TR_LIST) {
-          __syncthreads();
-          if (threadIdx.x == 0) sh.listed = 0;
-          __syncthreads();
-          each([&](u64 at) { const uint32_t i = atomicAdd(&sh.listed, 1u); if (i < TR_LIST) sh.list[i] = at; });
-          __syncthreads();
-          listed = true;
+      if (from_list) {
+        const uint32_t listed = sh.listed;
+#pragma unroll 1
+        for (uint32_t i = threadIdx.x; i < listed; i += NT) {
+          const u64 at = sh.list[i];
+          if (mode == LAST) {
+            const bool on = at >= lo && at <= hi;
+            const u64 mask = __ballot(on);
+            if (!mask) continue;
+            const int leader = __ffsll(mask) - 1;
+            uint32_t to = 0;
+            if (lane == leader) to = atomicAdd(&sh.few, (uint32_t)__popcll(mask));
+            to = __builtin_amdgcn_readlane(to, leader) + __popcll(mask & ((1ull << lane) - 1));
+            if (on && to < TR_LAST) { sh.fine_mass[to] = at; sh.fine_mass[TR_LAST + to] = wt.number(logit_of(at)); }
+          } else {
+            take(at, logit_of(at));
+          }
         }
-        if (n <= 64) break;
-        u64 least = ~0ull, most = 0;
-        each([&](u64 at) { least = min(least, at); most = max(most, at); });
+      } else {
+        // A wave takes 4 x 64 of the 16s at a time and, of those whose maxima are not behind the last bin, a quad a lane.  What is taken of the quads
+        // lies between two logits a little outside of the bins: tokens behind the last bin are no matter, those before the first one are left out by it.
+        const float d_last = last == TR_BINS - 1 ? INFINITY : (float)(last + 1) / sc.per_unit, d_first = first ? (float)first / sc.per_unit : 0.f;
+        const float low = sc.endless ? INFINITY : fmaxf(sc.zero - d_last - 1e-6f * (fabsf(sc.zero) + d_last), -3.4028235e38f);
+        const float high = sc.endless ? INFINITY : sc.zero - d_first + 1e-6f * (fabsf(sc.zero) + d_first);
+        const bool all = first == 0 && lo == 0 && hi == ~0ull;
+#pragma unroll 1
+        for (int g0 = 256 * wv; g0 < a.n16; g0 += 256 * Sh::WAVES) {
+          int order[4], hits[4], rounds = 0;
+          float z16[4];
 #pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) { least = min(least, (u64)__shfl_xor(least, o, 64)); most = max(most, (u64)__shfl_xor(most, o, 64)); }
-        __syncthreads();
-        if (lane == 0) { sh.wave_u[0][wv] = least; sh.wave_u[1][wv] = most; }
-        for (int i = threadIdx.x; i < TR_FINE; i += NT) { sh.fine_mass[i] = 0; sh.fine_cnt[i] = 0; }
+          for (int i = 0; i < 4; ++i) z16[i] = max16[min(g0 + 64 * i + lane, a.n16 - 1)];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const bool hit = g0 + 64 * i + lane < a.n16 && z16[i] >= low && z16[i] > -INFINITY;
+            const u64 mask = __ballot(hit);
+            const int before = __popcll(mask & ((1ull << lane) - 1));
+            hits[i] = __popcll(mask);
+            order[i] = __builtin_amdgcn_ds_permute(4 * (hit ? before : hits[i] + lane - before), lane);  // those first
+            rounds = max(rounds, (hits[i] + 15) / 16);
+          }
+          Quad<T, VEC> ahead[4];
+          int ahead_x[4];
+          auto load = [&](int round) {
+            const int nth = 16 * round + (lane >> 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int g = g0 + 64 * i + __builtin_amdgcn_ds_bpermute(4 * nth, order[i]);
+              ahead_x[i] = nth < hits[i] ? 16 * g + 4 * (lane & 3) : V;  // (V: none)
+              ahead[i].load(z_row, ahead_x[i], V);
+            }
+          };
+          load(0);
+#pragma unroll 1
+          for (int round = 0; round < rounds; ++round) {
+            Quad<T, VEC> v[4];
+            int x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[i] = ahead[i]; x[i] = ahead_x[i]; }
+            load(round + 1);  // (behind the last one: none)
+            float z[4][4];
+            int in[4], own = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              in[i] = 0;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                z[i][e] = Conv<T>::ld(v[i].v, e);
+                in[i] |= (z[i][e] >= low && z[i][e] <= high && (VEC || x[i] + e < V)) << e;
+              }
+              if (x[i] >= V) in[i] = 0;
+              if (sc.endless) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) z[i][e] = sc.of(z[i][e]);
+              }
+              if (!all && in[i]) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const u64 at = place_of(z[i][e], x[i] + e);
+                  in[i] &= ~((sc.bin(z[i][e]) < first || at < lo || at > hi) << e);
+                }
+              }
+              own += __popc(in[i]);
+            }
+            if (mode == LIST) {
+              const uint32_t upto = sum_to_lane((uint32_t)own), whole = __builtin_amdgcn_readlane(upto, 63);
+              if (!whole) continue;
+              uint32_t to = 0;
+              if (lane == 63) to = atomicAdd(&sh.listed, whole);
+              to = __builtin_amdgcn_readlane(to, 63) + upto - own;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                if (!in[i]) continue;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (in[i] >> e & 1) {
+                    if (to < Sh::LIST) sh.list[to] = place_of(z[i][e], x[i] + e);
+                    ++to;
+                  }
+              }
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+#pragma unroll 1
+                for (int e = 0; e < 4; ++e)
+                  if (in[i] >> e & 1) {
+                    const float y = e == 0 ? z[i][0] : e == 1 ? z[i][1] : e == 2 ? z[i][2] : z[i][3];
+                    take(place_of(y, x[i] + e), y);
+                  }
+              }
+            }
+          }
+        }
+      }
+      __syncthreads();
+      if (mode == LIST) {
+        n = sh.listed;
+        from_list = n <= Sh::LIST;
+        all_listed = lo == 0 && first == 0;
+        if (r.few && !by_mass && n <= (uint32_t)k && from_list && all_listed) {  // fewer finite ones than asked for, or just as many
+          target = n;
+          searching = n > 0;
+        }
+      } else if (mode == BOUNDS) {
+        least = ~max_to_lane(~least);
+        most = max_to_lane(most);
+        if (lane == 63) { sh.wave_u[0][wv] = least; sh.wave_u[1][wv] = most; }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < NT / 64; ++i) { least = min(least, sh.wave_u[0][i]); most = max(most, sh.wave_u[1][i]); }
-        lo = least; hi = most;
-        const int bits = 64 - __clzll(hi - lo), sh_r = max(0, bits - 8);
-        each([&](u64 at) {
-          const int bin = (int)((at - lo) >> sh_r);
-          atomicAdd(&sh.fine_cnt[bin], 1u);
-          atomicAdd(&sh.fine_mass[bin], wt.number(wt.log2_of(logit_of(at))));
-        });
+        lo = base = least;
+        hi = most;
+        parts_to(hi);
+      } else if (mode == PARTS) {
+        int part;
+        searching = find_bin<NT, TR_FINE>(sh, sh.fine_cnt, sh.fine_mass, by_mass, target, bc, bm, part, n);
+        const u64 begin = base + ((u64)part << drop);
+        if (part > 0) lo = max(lo, begin);
+        if (part < TR_FINE - 1) hi = min(hi, begin + ((1ull << drop) - 1));
+        bounded = false;
+      } else if (mode == SUM) {
+        uint32_t c = 0;
+        scan<NT>(sh, c, sum, all_c, all_m);
+        target = part_of(all_m);
+        bc = 0; bm = 0; n = min((uint32_t)k, n);
+        summing = false;
+      } else {
+        // Few tokens: four threads each, which add up those of a quarter of them that come up to it.  (Their sums go where none of the others' is read.)
+        if (threadIdx.x == 0) sh.found_place = ~0ull;
+        for (int i = threadIdx.x; i < TR_LAST; i += NT) { sh.fine_cnt[i] = bc; sh.last_mass[i] = bm; }
         __syncthreads();
-        int bin;
-        if (!find_bin<NT, TR_FINE>(sh, sh.fine_cnt, sh.fine_mass, by_mass, target, before_cnt, before_mass, bin, n)) break;
-        lo += (u64)bin << sh_r;
-        hi = lo + min(hi - lo, (1ull << sh_r) - 1);
-      }
-      __syncthreads();
-      if (threadIdx.x == 0) { sh.found_place = ~0ull; sh.found_cnt = before_cnt; sh.found_mass = before_mass; }
-      // 64 tokens at most: a lane each, which adds up those up to its own
-      if (wv == 0) {
-        u64 mine = ~0ull;
-        const uint32_t listed_n = min(sh.listed, (uint32_t)TR_LIST);
-        n = min(n, 64u);
-        uint32_t have = 0;
-        for (uint32_t i = 0; i < listed_n; i += 64) {  // (all of them, of which n lie in the interval)
-          const u64 at = i + lane < listed_n ? sh.list[i + lane] : ~0ull;
-          const u64 in = __ballot(at >= lo && at <= hi && i + lane < listed_n);
-          const uint32_t rank = have + __popcll(in & ((1ull << lane) - 1));
-          if (in >> lane & 1 && rank < 64) sh.fine_mass[rank] = at;
-          have += __popcll(in);
+        const int some = (int)min(sh.few, (uint32_t)TR_LAST);
+        for (int i = threadIdx.x; i < 4 * TR_LAST; i += NT) {
+          const int of = i % TR_LAST, j0 = i / TR_LAST * (TR_LAST / 4);
+          if (of >= some || j0 >= some) continue;
+          const u64 own = sh.fine_mass[of];
+          uint32_t c = 0;
+          u64 m = 0;
+#pragma unroll 1
+          for (int j = j0; j < min(some, j0 + TR_LAST / 4); j += 8) {
+            u64 other[8], w[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) { other[e] = sh.fine_mass[j + e]; w[e] = sh.fine_mass[TR_LAST + j + e]; }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const bool upto = j + e < some && other[e] <= own;
+              c += upto;
+              m += upto ? w[e] : 0;
+            }
+          }
+          atomicAdd(&sh.fine_cnt[of], c);
+          atomicAdd(&sh.last_mass[of], m);
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (lane < (int)n) mine = sh.fine_mass[lane];
-        const u64 w = lane < (int)n ? wt.number(wt.log2_of(logit_of(mine))) : 0;
-        uint32_t c = before_cnt;
-        u64 m = before_mass;
-        for (int j = 0; j < (int)n; ++j) {
-          const u64 other = __shfl(mine, j, 64), ow = __shfl(w, j, 64);
-          if (other <= mine) { ++c; m += ow; }
+        __syncthreads();
+        if ((int)threadIdx.x < some) {
+          const u64 m = sh.last_mass[threadIdx.x], to = by_mass ? m : sh.fine_cnt[threadIdx.x];
+          if (to >= target && to - (by_mass ? sh.fine_mass[TR_LAST + threadIdx.x] : 1) < target) { sh.found_place = sh.fine_mass[threadIdx.x]; sh.found_mass = m; }
         }
-        const u64 is = by_mass ? m : c, was = is - (by_mass ? w : 1);
-        if (lane < (int)n && was < target && is >= target) { sh.found_place = mine; sh.found_cnt = c; sh.found_mass = m; }
+        __syncthreads();
+        border = sh.found_place;
+        searching = r.by_p && !by_mass && border != ~0ull;
+        by_mass = true;
+        if (searching && r.few) {
+          lo = 0; hi = border;  // of the first k the sum, and its part
+          n = (uint32_t)k;
+          from_list = from_list && all_listed;
+          base = place_of(sc.zero, 0);
+          parts_to(border);
+          summing = true;
+        } else if (searching) {
+          target = part_of(sh.found_mass);  // (reached among the first k at the latest: the bins need not know of them)
+          searching = look_at_bin();
+          parts_of_bins();
+        }
       }
-      __syncthreads();
-      before_cnt = sh.found_cnt; before_mass = sh.found_mass;
-      return sh.found_place;
-    };
-
-    int bin;
-    uint32_t n, bc = 0;
-    u64 bm = 0;
-    if (k > 0 && (uint32_t)k < all_c) {
-      find_bin<NT, TR_BINS>(sh, sh.cnt, sh.mass, false, (u64)k, bc, bm, bin, n);
-      border = resolve(bin, n, false, (u64)k, bc, bm);
-      all_m = bm;
-    }
-    if (p < 1.f) {
-      const u64 target = max((u64)1, min(all_m, (u64)ceil(fmax((double)p, 0.) * (double)all_m)));
-      bc = 0; bm = 0;
-      __syncthreads();
-      find_bin<NT, TR_BINS>(sh, sh.cnt, sh.mass, true, target, bc, bm, bin, n);
-      border = resolve(bin, n, true, target, bc, bm);
     }
   }
-  // as a logit and, among equal ones, a token
-  const float last_z = border == ~0ull ? -INFINITY : logit_of(border);
-  const int last_id = border == ~0ull ? -1 : (int)(uint32_t)border;
-  const bool floored = floor_p > 0.f;
-  const double least = floored ? log2((double)fminf(floor_p, 1.f)) : 0.;
-  auto kept = [&](float z, int id) { return (z > last_z || (z == last_z && id <= last_id)) && (!floored || wt.log2_of(z) >= least); };
-  const float zero = endless ? 0.f : top;
 
-  const int steps = (V + 4 * NT - 1) / (4 * NT), per = (steps + TR_SEGS - 1) / TR_SEGS;
-  const bool in_place = (const void *)out == (const void *)z_row;
-  if (a.tokens) __syncthreads();
-  auto finish = [&](bool write, bool add) {
-    for (int step = 0; step < steps; ++step) {
-      const int x = 4 * (step * NT + threadIdx.x);
-      float z[4];
-      fetch(x, z);
-      u64 w = 0;
-      float y[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        y[i] = -INFINITY;
-        if (kept(z[i], x + i)) {
-          if (add) w += wt.number(wt.log2_of(z[i]));
-          y[i] = (z[i] - zero) / temp;
-        }
-      }
-      if (write) {
-        if constexpr (VEC) {
-          if (x < V) *(float4 *)(out + x) = make_float4(y[0], y[1], y[2], y[3]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (x + i < V) out[x + i] = y[i];
-        }
-      }
-      if (add && __any(w != 0)) {
-        w = wave_sum(w);
-        if (lane == 0) atomicAdd(&sh.seg[step / per], w);
-      }
-    }
-  };
-  if (out && !(in_place && a.tokens)) finish(true, a.tokens != nullptr);
-  else finish(false, true);
-  if (!a.tokens) return;
-
-  // the draw: the first token with which the sum of the kept weights, in the order of ids, exceeds u times their total
+  // The border as a logit and, among equal ones, a token: kept is what is larger, or equal and not behind it.
+  float last_z = border == ~0ull ? -INFINITY : logit_of(border);
+  int last_id = border == ~0ull ? -1 : (int)(uint32_t)border;
+  if (r.floor_p > 0.f && wt.c > 0.) {
+    // min-p as a border: the lowest logit whose weight is enough, which is next to what the logarithm gives, and the largest logit at most
+    const double least = log2((double)fminf(r.floor_p, 1.f));
+    float z = nextafterf(nextafterf((float)(wt.M + least / wt.c), -INFINITY), -INFINITY);
+    for (int i = 0; i < 6 && !(wt.log2_of(z) >= least); ++i) z = nextafterf(z, INFINITY);
+    z = fminf(z, sc.zero);
+    if (z > last_z) { last_z = nextafterf(z, -INFINITY); last_id = -1; }
+  }
+  const bool draw = a.tokens && border != ~0ull && from_list && all_listed;
+  if (threadIdx.x == 0) a.border[row] = RowBorder{wt.c, last_z, sc.zero, r.temp, last_id, sc.endless, draw};
+  if (!draw) return;
   __syncthreads();
-  u64 total = 0;
-  for (int i = 0; i < TR_SEGS; ++i) total += sh.seg[i];
-  const double want = (double)a.u[row] * (double)total;
-  const u64 target = want > 0. ? min(total - 1, (u64)want) : 0;  // exceeded from target + 1 on
-  u64 before = 0;
-  int seg = 0;
-  while (seg < TR_SEGS - 1 && before + sh.seg[seg] <= target) before += sh.seg[seg++];
-  for (int step = seg * per; step < min(steps, seg * per + per); ++step) {
-    const int x = 4 * (step * NT + threadIdx.x);
-    float z[4];
-    fetch(x, z);
-    u64 w[4], to = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      w[i] = kept(z[i], x + i) ? wt.number(wt.log2_of(z[i])) : 0;
-      to += w[i];
-    }
-    uint32_t c = 0, all_c;
-    u64 all, at = before - to;
-    scan<NT>(sh, c, to, all_c, all);
-    at += to;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (at <= target && at + w[i] > target) a.tokens[row] = x + i;
-      at += w[i];
-    }
-    before += all;
-    if (before > target) break;
+  for (int i = threadIdx.x; i < Sh::UNITS; i += NT) sh.mass[i] = 0;
+  __syncthreads();
+  const Kept kept{last_z, last_id};
+  const int per = (a.stretches + Sh::UNITS - 1) / Sh::UNITS;
+  for (uint32_t i = threadIdx.x; i < sh.listed; i += NT) {
+    const u64 at = sh.list[i];
+    const int id = (int)(uint32_t)at;
+    if (kept(logit_of(at), id)) atomicAdd(&sh.mass[(id >> 8) / per], wt.number(logit_of(at)));
   }
-  if (out && in_place) {
-    __syncthreads();
-    finish(true, false);
+  __syncthreads();
+  draw_token<T, VEC, NT>(sh, a, row, sc, kept, sh.mass, Sh::UNITS, per);
+}
+
+// ------------------------------------------------------------------ the result
+template <class T, bool VEC>
+__global__ __launch_bounds__(256) void k_row_finish(TruncateArgs a, int pieces, bool write, bool add) {
+  const int row = a.row0 + blockIdx.x / pieces, piece = blockIdx.x % pieces, V = a.V, lane = threadIdx.x & 63;
+  const T *z_row = (const T *)a.logits + (int64_t)row * a.row_stride;
+  const float *max16 = a.max16 + (int64_t)row * a.n16;
+  float *out = write ? a.out + (int64_t)row * V : nullptr;
+  const RowBorder rb = a.border[row];
+  const Kept kept{rb.last_z, rb.last_id};
+  const Weights wt{(double)rb.zero, rb.c, a.shift};
+  add = add && !rb.drawn;
+  if (!write && !add) return;
+  const int x0 = piece * 4096 + 4 * threadIdx.x;
+  float top[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) top[i] = max16[min(x0 + 1024 * i, V - 1) >> 4];
+  Quad<T, VEC> v[4];
+  bool some[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float t = !rb.endless ? top[i] : top[i] == INFINITY ? 0.f : -INFINITY;
+    some[i] = t >= rb.last_z && t > -INFINITY;
+    if (some[i]) v[i].load(z_row, x0 + 1024 * i, V);
   }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int x = x0 + 1024 * i;
+    if (x - 4 * lane >= V) break;
+    float y[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    u64 w = 0;
+    if (some[i]) {
+      float z[4];
+      v[i].numbers(x, V, z);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (rb.endless) z[e] = z[e] == INFINITY ? 0.f : -INFINITY;
+        if (kept(z[e], x + e)) {
+          y[e] = (z[e] - rb.zero) / rb.temp;
+          if (add) w += wt.number(z[e]);
+        }
+      }
+    }
+    if (add) {
+      if (__any(w != 0)) w = sum_to_lane(w);
+      if (lane == 63) a.sums[(int64_t)row * a.stretches + (x >> 8)] = w;
+    }
+    if (write) {
+      if constexpr (VEC) {
+        if (x < V) *(float4 *)(out + x) = make_float4(y[0], y[1], y[2], y[3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (x + e < V) out[x + e] = y[e];
+      }
+    }
+  }
+}
+
+template <class T, bool VEC>
+__global__ __launch_bounds__(256) void k_row_draw(TruncateArgs a) {
+  __shared__ DrawShared<256> sh;
+  const int row = a.row0 + blockIdx.x;
+  const RowBorder rb = a.border[row];
+  if (rb.drawn) return;
+  const RowScale sc(a, row, rb.temp);
+  draw_token<T, VEC, 256>(sh, a, row, sc, Kept{rb.last_z, rb.last_id}, a.sums + (int64_t)row * a.stretches, a.stretches, 1);
 }
 
 }  // namespace spec
@@ -427,12 +857,39 @@ static int truncate_check(const char *who, int32_t B, int32_t s, int32_t vocab) 
   return SPEC_OK;
 }
 
+// The pieces of a call's rows and where the workspace has what; -> its bytes.
+static size_t truncate_layout(TruncateArgs &a, int64_t rows, void *workspace) {
+  const int V = a.V;
+  auto up = [](int64_t n, int64_t to) { return (n + to - 1) / to; };
+  a.piece = (int)(up(up(V, 4096), TR_PIECES) * 4096);
+  a.pieces = (int)up(V, a.piece);
+  // bins cost 24 KB a piece, written and read again: as many pieces as it takes to fill the chip, of 4096 tokens at least
+  a.cuts = (int)std::max<int64_t>(1, std::min(up(V, 4096), up(1024, std::max<int64_t>(1, rows))));
+  a.cuts = (int)up(V, up(V, (int64_t)a.cuts * 4096) * 4096);
+  a.n16 = (int)up(V, 16);
+  a.stretches = (int)up(V, 256);
+  size_t at = 0;
+  auto take = [&](auto *&p, size_t n) {
+    p = (std::remove_reference_t<decltype(p)>)((char *)workspace + at);
+    at += (n * sizeof(*p) + 255) / 256 * 256;
+  };
+  take(a.piece_max, rows * TR_PIECES);
+  take(a.max16, rows * a.n16);
+  take(a.border, rows);
+  take(a.sums, rows * a.stretches);
+  take(a.masses, rows * a.cuts * TR_BINS);
+  take(a.counts, rows * a.cuts * TR_BINS);
+  return at;
+}
+
 extern "C" int spec_truncate_logits_workspace_bytes(int32_t B, int32_t s, int32_t vocab, size_t *bytes) {
   const char *who = "spec_truncate_logits_workspace_bytes";
   if (!bytes) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: bytes is null", who);
   const int rc = truncate_check(who, B, s, vocab);
   if (rc) return rc;
-  *bytes = 0;
+  TruncateArgs a{};
+  a.V = vocab;
+  *bytes = truncate_layout(a, (int64_t)B * (s + 1), nullptr);
   return SPEC_OK;
 }
 
@@ -449,20 +906,45 @@ extern "C" int spec_truncate_logits(void *hip_stream, const void *d_logits, int3
   if (!d_logits || (!d_out && !d_tokens)) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: null pointer", who);
   if (d_tokens && !d_uniforms) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: tokens need d_uniforms", who);
   if (((uintptr_t)d_logits % dtype_bytes(dtype)) || ((uintptr_t)d_out & 3)) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: misaligned pointer", who);
-  if ((const void *)d_out == d_logits && (dtype != SPEC_DTYPE_F32 || row_stride != vocab))
+  const bool in_place = (const void *)d_out == d_logits;
+  if (in_place && (dtype != SPEC_DTYPE_F32 || row_stride != vocab))
     return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: in place only for fp32 rows without padding", who);
   int bits = 0;
   while (bits < 28 && (1 << bits) < vocab) ++bits;
-  TruncateArgs a{d_logits, row_stride, s + 1, vocab, std::min(50, 62 - bits), rules->d_temperature, rules->d_top_k, rules->d_top_p, rules->d_min_p,
+  const int rows = B * (s + 1);
+  TruncateArgs a{d_logits, row_stride, 0, s + 1, vocab, std::min(50, 62 - bits), rules->d_temperature, rules->d_top_k, rules->d_top_p, rules->d_min_p,
                  d_out, d_uniforms, d_tokens};
+  a.B = B;
+  const size_t need = truncate_layout(a, rows, d_workspace);
+  if (!d_workspace || ((uintptr_t)d_workspace & 255) || workspace_bytes < need)
+    return fail_noctx(SPEC_ERR_WORKSPACE, "%s: workspace null, not 256-byte aligned, or smaller than %zu bytes", who, need);
+  hipStream_t st = (hipStream_t)hip_stream;
+  const int fours = (vocab + 4095) / 4096;
+  const int most = std::max(1, ((1 << 24) - 1) / std::max(fours, 4));  // rows of a launch: a grid holds less than 2^32 threads
   SPEC_DISPATCH_DTYPE(dtype, T, {
     const bool vec = vocab % 4 == 0 && row_stride % 4 == 0 && (uintptr_t)d_logits % (4 * sizeof(T)) == 0 && (uintptr_t)d_out % 16 == 0;
-    if (vocab > 8192)
-      hipLaunchKernelGGL((vec ? k_truncate_logits<T, true, 1024> : k_truncate_logits<T, false, 1024>), dim3(B * (s + 1)), dim3(1024), 0,
-                         (hipStream_t)hip_stream, a);
-    else
-      hipLaunchKernelGGL((vec ? k_truncate_logits<T, true, 256> : k_truncate_logits<T, false, 256>), dim3(B * (s + 1)), dim3(256), 0,
-                         (hipStream_t)hip_stream, a);
+    auto launch = [&](auto VEC_) {
+      constexpr bool VEC = decltype(VEC_)::value;
+      auto each = [&](auto f) {  // launches of up to `most` rows
+        for (a.row0 = 0; a.row0 < rows; a.row0 += most) f((unsigned)std::min(most, rows - a.row0));
+        a.row0 = 0;
+      };
+      const bool first = d_out && !(in_place && d_tokens);  // (in place the draw reads the row before it goes)
+      each([&](unsigned n) { hipLaunchKernelGGL((k_row_maxima<T, VEC>), dim3(n * a.pieces), dim3(256), 0, st, a); });
+      if (rules->d_top_p || rules->d_top_k) {
+        if (B <= 64) hipLaunchKernelGGL((k_row_masses<T, VEC>), dim3(rows * a.cuts), dim3(512), 0, st, a);
+        else each([&](unsigned n) { hipLaunchKernelGGL((k_row_masses<T, VEC>), dim3(n * a.cuts), dim3(512), 0, st, a); });
+      }
+      each([&](unsigned n) {
+        if (vocab > 8192) hipLaunchKernelGGL((k_row_border<T, VEC, 512>), dim3(n), dim3(512), 0, st, a);
+        else hipLaunchKernelGGL((k_row_border<T, VEC, 256>), dim3(n), dim3(256), 0, st, a);
+      });
+      each([&](unsigned n) { hipLaunchKernelGGL((k_row_finish<T, VEC>), dim3(n * fours), dim3(256), 0, st, a, fours, first, d_tokens != nullptr); });
+      if (d_tokens) each([&](unsigned n) { hipLaunchKernelGGL((k_row_draw<T, VEC>), dim3(n), dim3(256), 0, st, a); });
+      if (d_out && !first) each([&](unsigned n) { hipLaunchKernelGGL((k_row_finish<T, VEC>), dim3(n * fours), dim3(256), 0, st, a, fours, true, false); });
+    };
+    if (vec) launch(std::true_type());
+    else launch(std::false_type());
   });
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? SPEC_OK : fail_noctx(SPEC_ERR_HIP, "%s: %s", who, hipGetErrorString(e));

@@ -261,3 +261,26 @@ def test_a_round_of_mixed_requests(B):
         for j in range(int(accepted[b]) + 1):
             assert p[b, j, emitted[b, j]] > -math.inf
     assert len(set(accepted.tolist())) > 1
+
+
+@pytest.mark.parametrize("nB,V", [(1, 40000), (64, 9000), (70, 9000), (300, 500)])
+def test_batches_whose_sequences_differ(B, nB, V):
+    """One sequence that needs sums over all tokens among others that do not, all, and none; more sequences than a wave has lanes."""
+    g = torch.Generator().manual_seed(nB)
+    z = logits_of(nB, 2, V, torch.bfloat16, seed=nB)
+    pick = lambda *v: [v[int(i)] for i in torch.randint(0, len(v), (nB,), generator=g)]
+    run(B, z, temperature=pick(0.0, 0.7, 1.3), top_k=pick(0, 3, 200, 1500, V - 1), top_p=pick(1.0, 0.3, 0.95), min_p=pick(0.0, 0.05))
+    run(B, z, top_p=[0.9 if b == nB // 2 else 1.0 for b in range(nB)])
+    run(B, z, top_k=[40] * nB)
+    run(B, z, min_p=[0.01] * nB)
+
+
+def test_more_tokens_in_a_bin_than_the_list_holds(B):
+    """Thousands of tokens of nearly the same weight around the border: narrowed down over the row."""
+    V = 60000
+    g = torch.Generator().manual_seed(77)
+    z = 5 + 1e-3 * torch.rand((4, 1, V), generator=g)
+    z[:, :, ::7] -= 9 * torch.rand((4, 1, (V + 6) // 7), generator=g)
+    run(B, z.to(DEV), top_k=[0, 900, 30000, 50000], top_p=[0.4, 0.7, 0.9, 1.0])
+    half = z.to(torch.bfloat16)  # the same in few distinct values
+    run(B, half.to(DEV), top_k=[0, 900, 30000, 50000], top_p=[0.4, 0.7, 0.9, 1.0])

@@ -109,8 +109,8 @@ def test_the_reference_agrees_with_torch_about_e4m3(td):
 
 
 def test_truncation_arguments(B):
-    def call(rules=True, logits=FAKE, dtype=B.DTYPE_F32, stride=1000, nB=2, s=3, V=1000, u=FAKE, out=FAKE + 64, tokens=FAKE):
-        return B.lib.spec_truncate_logits(None, logits, dtype, stride, nB, s, V, C.byref(B.SamplingRulesDesc()) if rules else None, u, None, 0, out, tokens)
+    def call(rules=True, logits=FAKE, dtype=B.DTYPE_F32, stride=1000, nB=2, s=3, V=1000, u=FAKE, ws=None, wb=0, out=FAKE + 64, tokens=FAKE):
+        return B.lib.spec_truncate_logits(None, logits, dtype, stride, nB, s, V, C.byref(B.SamplingRulesDesc()) if rules else None, u, ws, wb, out, tokens)
     for kw in (dict(nB=-1), dict(s=-1), dict(V=0), dict(dtype=7), dict(stride=999), dict(rules=False), dict(logits=None), dict(out=None, tokens=None),
                dict(u=None), dict(logits=FAKE + 2), dict(out=FAKE + 2), dict(dtype=B.DTYPE_BF16, out=FAKE), dict(stride=1004, out=FAKE)):
         assert call(**kw) == B.ERR_INVALID_ARG, kw
@@ -119,7 +119,10 @@ def test_truncation_arguments(B):
         assert call(**kw) == B.ERR_CAPACITY, kw
     assert call(nB=0, logits=None, out=None, tokens=None) == B.OK
     n = C.c_size_t(1)
-    assert B.lib.spec_truncate_logits_workspace_bytes(1, 0, 32000, C.byref(n)) == B.OK
+    assert B.lib.spec_truncate_logits_workspace_bytes(2, 3, 1000, C.byref(n)) == B.OK and n.value > 1
+    for kw in (dict(), dict(ws=FAKE + 16, wb=n.value), dict(ws=FAKE, wb=n.value - 1)):
+        assert call(**kw) == B.ERR_WORKSPACE
+    assert B.lib.spec_truncate_logits_workspace_bytes(65535, 15, 1 << 28, C.byref(n)) == B.OK
     assert B.lib.spec_truncate_logits_workspace_bytes(1, 16, 32000, C.byref(n)) == B.ERR_CAPACITY
     assert B.lib.spec_truncate_logits_workspace_bytes(1, 0, 0, C.byref(n)) == B.ERR_INVALID_ARG
     assert B.lib.spec_truncate_logits_workspace_bytes(1, 0, 10, None) == B.ERR_INVALID_ARG
