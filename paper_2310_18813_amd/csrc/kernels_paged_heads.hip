@@ -98,7 +98,20 @@ __global__ __launch_bounds__(256) void k_paged_heads(HeadArgs a) {
   constexpr int E = Unit<T>::E, ITEMS = HD / (2 * E);
   __shared__ float2 turn[HD / 2];
   __shared__ double2 turn64[C8 ? HD / 2 : 1];
-  const int row = blockIdx.x;
+  const int row = blockIdx.x, item = (int)blockIdx.y * 256 + (int)threadIdx.x, head = item / ITEMS, u = item % ITEMS;
+  const int Hk = a.p.n_kv_heads, hu = a.half / E;  // hu: items of a head that turn
+  const bool on = head < a.n_q + 2 * Hk, is_q = head < a.n_q, is_v = head >= a.n_q + Hk;  // (on: all lanes of a head at once)
+  const int h = is_q ? head : is_v ? head - a.n_q - Hk : head - a.n_q;
+  const bool turns = !is_v && u < hu;
+  const int u0 = turns && !a.interleaved ? u : 2 * u, u1 = turns && !a.interleaved ? u + hu : u0 + 1;
+  // the loads first: whether anything comes of them takes three loads after one another, and the angles
+  u32x4_v x0, x1;
+  if (on) {
+    const unsigned char *src = is_q ? a.q + (row * a.q_stride + h * HD) * sizeof(T)
+                                    : is_v ? a.v + (row * a.v_stride + h * HD) * sizeof(T) : a.k + (row * a.k_stride + h * HD) * sizeof(T);
+    x0 = ((const u32x4_v *)src)[u0];
+    x1 = ((const u32x4_v *)src)[u1];
+  }
   const int b = __builtin_amdgcn_readfirstlane(row_sequence(a.p, row));
   if (b >= a.p.B) return;
   const PagedSeq s = paged_seq(a.p, b);
@@ -107,9 +120,9 @@ __global__ __launch_bounds__(256) void k_paged_heads(HeadArgs a) {
   const int page = paged_page(a.p, b, pos);
   if ((int)threadIdx.x < a.half) {
     // the angle in turns, of which whole ones are left out
-    const double turns = (double)pos * a.inv_freq[threadIdx.x] * 0.15915494309189533577;
-    const double part = turns - rint(turns);
-    if constexpr (C8) {
+    const double angle = (double)pos * a.inv_freq[threadIdx.x] * 0.15915494309189533577;
+    const double part = angle - rint(angle);
+    if (C8 && (int)(blockIdx.y * 256 + 255) / ITEMS >= a.n_q) {  // (queries alone do with fp32)
       double sn, cs;
       sincospi(2. * part, &sn, &cs);
       turn64[threadIdx.x] = make_double2(cs, sn);
@@ -121,18 +134,7 @@ __global__ __launch_bounds__(256) void k_paged_heads(HeadArgs a) {
     }
   }
   __syncthreads();
-  const int item = (int)blockIdx.y * 256 + (int)threadIdx.x, head = item / ITEMS, u = item % ITEMS;
-  const int Hk = a.p.n_kv_heads;
-  if (head >= a.n_q + 2 * Hk) return;  // (all lanes of a head at once)
-  const bool is_q = head < a.n_q, is_v = head >= a.n_q + Hk;
-  if (!is_q && page < 0) return;
-  const int h = is_q ? head : is_v ? head - a.n_q - Hk : head - a.n_q;
-  const unsigned char *src = is_q ? a.q + (row * a.q_stride + h * HD) * sizeof(T)
-                                  : is_v ? a.v + (row * a.v_stride + h * HD) * sizeof(T) : a.k + (row * a.k_stride + h * HD) * sizeof(T);
-  const int hu = a.half / E;  // items of a head that turn
-  const bool turns = !is_v && u < hu;
-  const int u0 = turns && !a.interleaved ? u : 2 * u, u1 = turns && !a.interleaved ? u + hu : u0 + 1;
-  const u32x4_v x0 = ((const u32x4_v *)src)[u0], x1 = ((const u32x4_v *)src)[u1];
+  if (!on || (!is_q && page < 0)) return;
   const unsigned char *norm = is_q ? a.q_norm : is_v ? nullptr : a.k_norm;
   float x[2 * E], w[2 * E];
   auto unpack = [](const u32x4_v &lo, const u32x4_v &hi, float (&f)[2 * E]) {
@@ -166,8 +168,12 @@ __global__ __launch_bounds__(256) void k_paged_heads(HeadArgs a) {
         e = encode<T, ITEMS>(y, c0, c1);
       }
       unsigned char *dst = (is_v ? a.p.v : a.p.k) + paged_row(a.p, page, pos) + ((size_t)h * a.p.head_units << 4);
-      ((uint2 *)dst)[u0] = c0;
-      ((uint2 *)dst)[u1] = c1;
+      if (u1 == u0 + 1) {  // (units beside each other: all but half pairs)
+        ((uint4 *)dst)[u0 >> 1] = make_uint4(c0.x, c0.y, c1.x, c1.y);
+      } else {
+        ((uint2 *)dst)[u0] = c0;
+        ((uint2 *)dst)[u1] = c1;
+      }
       if (u == 0) (is_v ? a.p.v_scale : a.p.k_scale)[paged_scale(a.p, page, h, pos)] = (uint8_t)(e + 127);
       return;
     }
