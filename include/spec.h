@@ -398,7 +398,7 @@ typedef struct {
 } spec_sampling_rules;
 
 /* spec_truncate_logits: the rules on d_logits, [B][s+1] rows as of spec_process_logits (any type, padded).
-     d_out [B][s+1][vocab] fp32 or NULL: x of the tokens that are kept, -infinity for the others: what spec_sample_accept and spec_sample_tokens take with
+     d_out [B][s+1][vocab] fp32 or NULL: x of the tokens that are kept (-infinity where it leaves fp32), -infinity for the others: what spec_sample_accept and spec_sample_tokens take with
      temperature 1 (target and draft rows alike), and what the round's acceptance is then exact for.  May be d_logits itself where the type
      is fp32 and row_stride = vocab.
      d_tokens [B][s+1] or NULL (not both): a draw from the kept tokens with d_uniforms [B][s+1], numbers in [0, 1): the lowest id whose cumulative weight
@@ -521,7 +521,8 @@ typedef struct {
 /* spec_paged8_append: spec_paged_append_normed into a cache of 8 bits.  Of a position's head y (keys in 64 bits up to the rounding, values as they
    are): the scale is 2^e, e the least exponent, from -100 (bf16) or -15 (fp16) on, with max |y| <= 448 * 2^e; the codes are y / 2^e to nearest,
    ties to even.  Magnitudes over the type's largest number of four bits (fp16: 61440) become that number; a head with a NaN, or with a magnitude that
-   the type rounds to infinity, is NaN throughout.  Queries stay in the rows' type.
+   the type rounds to infinity, is NaN throughout.  Queries stay in the rows' type.  Two rows that the pages send to the same place may leave one's codes
+   under the other's scale there.
 
    spec_paged8_read: what the cache holds of the batch's rows, back in the rows' type (exactly): d_k, d_v [rows][n_kv_heads][head_dim], row strides in
    elements, alignment as above; NULL: not wanted (not both).  Zeros where a page is absent; dead rows and rows that no sequence owns are left as they were.

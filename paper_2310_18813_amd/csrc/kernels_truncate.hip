@@ -435,11 +435,13 @@ __global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
     }
     if (first != ~0u) atomicMin(&sh.few, first);
     __syncthreads();
-    if (threadIdx.x == 0) {
-      int id = 16 * (int)sh.few;
-      while (id < min(V, 16 * (int)sh.few + 15) && !(Conv<T>::ld(z_row, id) == sc.top)) ++id;
-      sh.list[0] = place_of(sc.zero, id);
-      sh.listed = 1;
+    if (wv == 0) {
+      const int id = 16 * (int)sh.few + (lane & 15);
+      const u64 mask = __ballot(id < V && Conv<T>::ld(z_row, min(id, V - 1)) == sc.top);
+      if (lane == 0) {
+        sh.list[0] = place_of(sc.zero, 16 * (int)sh.few + (mask ? __ffsll(mask) - 1 : 0));
+        sh.listed = 1;
+      }
     }
     __syncthreads();
     border = sh.list[0];
@@ -575,7 +577,7 @@ __global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
       } else {
         // A wave takes 4 x 64 of the 16s at a time and, of those whose maxima are not behind the last bin, a quad a lane.  What is taken of the quads
         // lies between two logits a little outside of the bins: tokens behind the last bin are no matter, those before the first one are left out by it.
-        const float d_last = last == TR_BINS - 1 ? INFINITY : (float)(last + 1) / sc.per_unit, d_first = first ? (float)first / sc.per_unit : 0.f;
+        const float d_last = last == TR_BINS - 1 ? INFINITY : (float)(last + 1) / sc.per_unit, d_first = first ? fminf((float)first / sc.per_unit, 3.4028235e38f) : 0.f;
         const float low = sc.endless ? INFINITY : fmaxf(sc.zero - d_last - 1e-6f * (fabsf(sc.zero) + d_last), -3.4028235e38f);
         const float high = sc.endless ? INFINITY : sc.zero - d_first + 1e-6f * (fabsf(sc.zero) + d_first);
         const bool all = first == 0 && lo == 0 && hi == ~0ull;
@@ -816,7 +818,8 @@ __global__ __launch_bounds__(256) void k_row_finish(TruncateArgs a, int pieces, 
       for (int e = 0; e < 4; ++e) {
         if (rb.endless) z[e] = z[e] == INFINITY ? 0.f : -INFINITY;
         if (kept(z[e], x + e)) {
-          y[e] = (z[e] - rb.zero) / rb.temp;
+          const float d = z[e] - rb.zero;
+          y[e] = d > -INFINITY ? d / rb.temp : (float)(((double)z[e] - rb.zero) / rb.temp);  // (the difference alone may leave fp32)
           if (add) w += wt.number(z[e]);
         }
       }

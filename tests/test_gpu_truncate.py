@@ -138,6 +138,10 @@ def test_narrow_and_wide_rows(B):
     run(B, near.to(DEV), top_k=[5000, 77, 0], top_p=[1.0, 0.6, 0.3])
     wide = torch.randn((3, 1, V), generator=g) * 1e38
     run(B, wide.to(DEV), temperature=[1.0, 1e38, math.inf], top_k=[5000, 1000, 0], top_p=[1.0, 0.9, 0.3])
+    ends = torch.full((3, 1, V), -3.2e38)  # differences beyond fp32, quotients within
+    ends[:, :, 7::11] = 3.3e38
+    out = run(B, ends.to(DEV), temperature=[1e38, 3e38, 1e35], top_k=[0, 5000, 0], top_p=[1.0, 1.0, 0.5])
+    assert out[:2] == [V, 5000]
     steep = torch.randn((2, 1, V), generator=g) * 200
     run(B, steep.to(DEV), top_k=[6000, 6000], top_p=[1.0, 0.999])
 
