@@ -16,6 +16,11 @@
 //                   its limit.  What the maxima rule out is not read.  Draws, where all that is kept is in the list.
 //   k_row_finish    the result; logits that the maxima rule out are not read.  Sums of the kept weights by 256 tokens, for
 //   k_row_draw      the other rows' draws.
+// 64 x 4 rows of 50272 bf16 logits, each sequence with its own rules: 9.6 + 15.4 + 34 + 16 + 4.6 us of 77; 24 x 8 fp32 rows of 151936: 28 + 16 + 52 + 28 + 5 of
+// 128; one row of 32000: 23.  The maxima and the result are at memory's rate (a copy's); the border is a chain of passes, 1.5 to 3 us
+// each from the list, and of trips to L2 where it reads the row: a workgroup a row, those whose border lies among all tokens last.  A
+// workgroup for all of a row took 113, 297 and 45: rows that need all their weights kept their CU while others had nothing to do.
+// What cost most in LDS: additions that return a place in a list, all to one word (3000 of them 30 us), so that a wave counts its tokens first.
 #include "spec_internal.h"
 #include "device_utils.h"
 #include <algorithm>
@@ -30,6 +35,9 @@ constexpr int TR_FINE = 256;   // parts that what is looked at is cut into
 constexpr int TR_LAST = 128;   // tokens that are put in order at once
 constexpr int TR_FEW = 1024;   // the largest top-k that goes by the maxima alone
 constexpr int TR_PIECES = 64;  // of a row, for its maxima
+// Pieces that a row with bins is cut into where few rows have bins: more fill the chip, but one workgroup reads the bins of all (16 KB each).  24 x 8 rows of
+// 151936, 64 x 4 of 50272, us: 8 pieces 127.7, 77.5; 12 129.6, 77.2; 24 129.4, 78.1; 37 (13) 132.2, 78.4.
+constexpr int TR_CUTS = 8;
 
 // What is found out about a row: kept is a logit that is larger than last_z, or equal with an id up to last_id; x = (z - zero) / temp.
 struct RowBorder {
@@ -334,7 +342,7 @@ struct Cuts {
     if (a.B <= 64) {
       const int lane = threadIdx.x & 63;
       dense = __ballot(lane < a.B && RowRules(a, min(lane, a.B - 1)).dense);
-      each = max(each, min((a.V + 4095) / 4096, a.B * a.cuts / max(1, __popcll(dense))));
+      each = max(each, min(min(TR_CUTS, (a.V + 4095) / 4096), a.B * a.cuts / max(1, __popcll(dense))));
     }
     cut = ((a.V + each * 4096 - 1) / (each * 4096)) * 4096;
     each = (a.V + cut - 1) / cut;

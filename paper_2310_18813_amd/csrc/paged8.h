@@ -32,7 +32,6 @@ __device__ __forceinline__ float to_odd(double v) {
   const uint32_t hi = (uint32_t)(u >> 32) | min((uint32_t)u, 1u);
   return (float)__builtin_bit_cast(double, (uint64_t)hi << 32);
 }
-__device__ __forceinline__ float to_odd(float v) { return v; }
 
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
 
