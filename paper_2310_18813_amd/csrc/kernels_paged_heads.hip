@@ -187,9 +187,9 @@ __global__ __launch_bounds__(256) void k_paged_heads(HeadArgs a) {
   u32x4_v y0 = x0, y1 = x1;
   if (norm || turns) {
     if (norm) {
-      const float rf = (float)r;
+      // (r itself leaves fp32 where x and eps are small)
 #pragma unroll
-      for (int i = 0; i < 2 * E; ++i) x[i] = x[i] * rf * w[i];
+      for (int i = 0; i < 2 * E; ++i) x[i] = (float)((double)x[i] * r) * w[i];
     }
     if (turns) rotate(x, turn + u * E, a.interleaved);
     float f0[E], f1[E];

@@ -211,6 +211,27 @@ def test_norms_of_large_and_of_zero_heads(B):
     assert torch.equal(c8.k.view(torch.uint8)[0, :3].cpu(), codes) and torch.equal(c8.k_scale[0, :, :3].t().cpu().long(), e + 127)
 
 
+@pytest.mark.parametrize("td", [torch.float32, torch.bfloat16, torch.float16])
+def test_norms_whose_root_is_beyond_fp32(B, td):
+    """eps 1e-80 and elements down to 2^-149: one over the root is up to 1e40, and a head of zeros stays zeros."""
+    hd = 64
+    x = torch.zeros((1, 4, hd), dtype=torch.float64)
+    x[0, 1] = torch.linspace(-1, 1, hd, dtype=torch.float64) * 2.0 ** (-12 if td is torch.float16 else -120)
+    x[0, 2, 5] = 2.0 ** (-24 if td is torch.float16 else -133 if td is torch.bfloat16 else -149)
+    x[0, 3] = 1e-6
+    x = x.to(td)
+    w = torch.ones(hd, dtype=td)
+    t = B.HeadTransform(None, False, w.to(DEV), w.to(DEV), 1e-80)
+    pages = [torch.zeros((1, 8, 4, hd), dtype=td, device=DEV) for _ in range(2)]
+    batch = B.PagedBatch(torch.zeros((1, 1), dtype=torch.int32, device=DEV), torch.ones(1, dtype=torch.int32, device=DEV), 1)
+    d = x.to(DEV)
+    q = B.spec_paged_append_normed(B.PagedCache(*pages), batch, d, d, d, t).cpu().double()[0]
+    want, e = ref.transform(x[0], 0, w, 1e-80, None, False)
+    e = e + ref.UNIT[td] * (want.abs() + e)
+    assert ((q - want).abs() <= e).all() and not q[0].any()
+    assert ((pages[0][0, 0].cpu().double() - want).abs() <= e).all()
+
+
 @pytest.mark.parametrize("norm", [False, True])
 def test_in_place_and_on_another_stream(B, norm):
     td, b = torch.bfloat16, ref.Batch([4, 4], [60, 33], 16, ragged=False)
