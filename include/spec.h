@@ -490,7 +490,7 @@ int spec_paged_attention(void *hip_stream, const spec_paged_cache *cache, const 
      y = x / sqrt(mean(x^2) + eps) * w, w = d_q_norm or d_k_norm ([head_dim], of the rows' type, 16-byte aligned; NULL: not normed)
      the first rope_dim elements turn by the angles p * d_inv_freq[i] (as in spec_paged_append), in pairs i and i + rope_dim / 2, or, interleaved = 1,
      2i and 2i + 1.
-   eps > 0 where there is a norm.  A NULL transform does nothing.  Sums of squares are 64 bits, products fp32, and one rounding ends it. */
+   eps > 0 where there is a norm.  A NULL transform does nothing.  The norm's sum, root and quotient are 64 bits, the products behind fp32, and one rounding ends it. */
 typedef struct {
   const double *d_inv_freq; /* [rope_dim / 2]; may be NULL where rope_dim is 0 */
   int32_t rope_dim;         /* a multiple of 16 up to head_dim                 */
@@ -508,7 +508,7 @@ int spec_paged_append_normed(void *hip_stream, const spec_paged_cache *cache, co
    infinities) at d_k[g * page_stride + p * pos_stride + h * head_stride + i] times 2^(d_k_scale[(g * n_kv_heads + h) * page_size + p] - 127);
    values likewise.  Strides in bytes, multiples of 16; d_k and d_v 16-byte aligned, the scales 8-byte aligned.  Sizes and limits otherwise as of
    spec_paged_cache; dtype is that of the row-wise tensors, SPEC_DTYPE_BF16 or SPEC_DTYPE_F16 (SPEC_ERR_UNSUPPORTED for fp32).
-   Half the bytes of a cache of 16 bits and one more a head: twice the positions in the same memory, half the time of attention over long contexts.
+   Half the bytes of a cache of 16 bits and one more a head: nearly twice the positions in the same memory, and attention of few rows in 0.6 of the time.
    An element is off by at most 1 / 16 of itself, or 2^-10 of its scale where that is more (2^-18 of the head's largest).  */
 typedef struct {
   int32_t dtype;

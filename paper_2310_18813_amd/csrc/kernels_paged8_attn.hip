@@ -11,7 +11,7 @@ extern "C" int spec_paged8_attention_workspace_bytes(const spec_paged_cache8 *ca
   if (!bytes) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: bytes is null", who);
   spec_paged_cache as;
   int rc = paged8_args(who, cache, batch, &as, &a.p);
-  if (!rc) rc = attend_check(who, &as, 1, batch, n_q_heads, 0, a, s);  // without a window: the largest need
+  if (!rc) rc = attend_check(who, &as, batch, n_q_heads, 0, a, s);  // without a window: the largest need
   if (rc) return rc;
   *bytes = attend_bytes(&as, s);
   return SPEC_OK;
@@ -27,7 +27,7 @@ extern "C" int spec_paged8_attention(void *hip_stream, const spec_paged_cache8 *
   spec_paged_cache as;
   int rc = paged8_args(who, cache, batch, &as, &a.p);
   if (!rc)
-    rc = attend_prepare(who, &as, 1, batch, n_q_heads, d_q, q_stride, scale, window, d_workspace, workspace_bytes, d_out,
+    rc = attend_prepare(who, &as, batch, n_q_heads, d_q, q_stride, scale, window, d_workspace, workspace_bytes, d_out,
                         out_stride, a, s, nothing);
   if (rc || nothing) return rc;
   if (s.qt == 16) {

@@ -10,7 +10,7 @@ extern "C" int spec_paged_attention_workspace_bytes(const spec_paged_cache *cach
   Shape s;
   if (!bytes) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: bytes is null", who);
   int rc = paged_args(who, cache, batch, &a.p);
-  if (!rc) rc = attend_check(who, cache, (int)dtype_bytes(cache->dtype), batch, n_q_heads, 0, a, s);  // without a window: the largest need
+  if (!rc) rc = attend_check(who, cache, batch, n_q_heads, 0, a, s);  // without a window: the largest need
   if (rc) return rc;
   *bytes = attend_bytes(cache, s);
   return SPEC_OK;
@@ -25,7 +25,7 @@ extern "C" int spec_paged_attention(void *hip_stream, const spec_paged_cache *ca
   bool nothing;
   int rc = paged_args(who, cache, batch, &a.p);
   if (!rc)
-    rc = attend_prepare(who, cache, (int)dtype_bytes(cache->dtype), batch, n_q_heads, d_q, q_stride, scale, window, d_workspace, workspace_bytes, d_out,
+    rc = attend_prepare(who, cache, batch, n_q_heads, d_q, q_stride, scale, window, d_workspace, workspace_bytes, d_out,
                         out_stride, a, s, nothing);
   if (rc || nothing) return rc;
   if (s.qt == 16) {

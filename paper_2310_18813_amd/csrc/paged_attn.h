@@ -12,6 +12,7 @@
 // positions, whole rows of a head across 16 lanes, and turns the block round in registers.
 // Few rows are bound by their loads: 64 sequences x 4 rows of 32 heads of 128 over up to 1000 positions, bf16, 650 MB in 125 us
 // (5.2 TB/s), and the loads without any arithmetic took as long.  Six sequences of up to 32000 positions, 32 heads over 8: 102 us.
+// The same over 8 bits, 329 MB: 74 us (4.4 TB/s; the loads without arithmetic 70).
 //
 // S, what the cache holds: the rows' type T, or e4m3 codes, which become numbers of T times their scale (exactly) on the way to the products:
 // keys and values of few rows in registers, those of many rows on their way to LDS.
@@ -319,12 +320,12 @@ template <bool C8> __device__ __forceinline__ void my_unit(int Hk, int &unit, in
 
 // ------------------------------------------------------------------ few query rows a tile: the waves share the positions
 // Workgroups that a CU holds at a time: by registers, which its launch bound holds the compiler to.
-constexpr int attend_resident(int dtype_bytes, int cached_bytes, int HD, int QT) {
+constexpr int attend_resident(int dtype_bytes, int HD, int QT) {
   if (dtype_bytes == 4) return HD == 64 && QT == 1 ? 3 : HD == 64 ? 2 : 1;
   return QT == 1 ? (HD == 64 ? 4 : 3) : QT == 2 ? (HD == 64 ? 3 : 1) : QT == 4 ? 1 : QT == 8 ? 2 : 1;
 }
 template <class T, class S, int HD, int QT>
-__global__ __launch_bounds__(256, attend_resident(sizeof(T), sizeof(S), HD, QT)) void k_paged_attend(AttendArgs a) {
+__global__ __launch_bounds__(256, attend_resident(sizeof(T), HD, QT)) void k_paged_attend(AttendArgs a) {
   typedef Step<T, S, HD> St;
   constexpr bool C8 = std::is_same<S, e4m3_t>::value;
   constexpr int R = 16 * QT, HT = HD / 16, KU = St::KU, VE = St::VE, LD = HD + 4;
@@ -606,7 +607,8 @@ __device__ __forceinline__ float max14(float top, const f32x16_v &x) {
 // the way to LDS.  The maximum follows the scores only when they have grown
 // by 2^8: weights up to 2^8 are as exact in 16 bits as weights up to 1 (fp16: up to 2^15 as those up to 2^7), the sums are fp32, and most tiles
 // then rescale nothing.
-// Chunks of up to 2048 rows over 8192 positions, 32 heads over 8, bf16: 417 us (913 TFLOP/s), products busy 42 % of the clocks.
+// Chunks of up to 2048 rows over 8192 positions, 32 heads over 8, bf16: 417 us (913 TFLOP/s), products busy 42 % of the clocks.  Of codes: 414 us; their
+// decoding, once for all rows of the workgroup, runs beside the products.
 constexpr int VALU = 0x2, MATRIX = 0x8, DS_READ = 0x100;  // kinds of instructions that sched_group_barrier tells apart
 constexpr int pc_lds(int NW) { return 4 * NW * 256 * 16; }
 
@@ -969,7 +971,7 @@ __global__ __launch_bounds__(256) void k_paged_join(AttendArgs a, int align) {
 }
 
 // The same with a wave a query row, whose four quarters take every fourth chunk: for a few rows that are cut into many chunks, which 16 lanes join one
-// after the other (one row of 32 heads over 8, 32000 positions in 63 chunks: 24 us).
+// after the other.  One row of 32 heads over 8, fp16, 32000 positions in 63 chunks of 8 bits: the join 22 -> 9 us, the call 38.1 -> 24.7.
 template <class T, int HD, int QT>
 __global__ __launch_bounds__(256) void k_paged_join_rows(AttendArgs a, int align) {
   constexpr int R = 16 * QT, VE = HD / 16, AHEAD = 8;
@@ -1036,7 +1038,7 @@ struct Shape {
 // where these make two rounds of workgroups and more.  us with 128 and with 256, bf16, 32 heads over 8: six sequences of 1000 rows (768 tiles of 256)
 // over up to 8192 positions 702 and 652 with heads of 128, 409 and 409 with heads of 64; one of 1500 (192 tiles) over 2048 positions
 // 68 and 66, 40 and 47; over 8192 253 and 219, 148 and 153.  So with few tiles heads of 64 gain from 128, heads of 128 would not need them.
-static Shape attend_shape(const spec_paged_cache *c, int cached_bytes, const spec_paged_batch *b, int n_q, int window) {
+static Shape attend_shape(const spec_paged_cache *c, const spec_paged_batch *b, int n_q, int window) {
   Shape s{};
   const int64_t Hk = c->n_kv_heads, G = n_q / Hk, per = (int64_t)b->max_rows * G;
   auto tiles = [&](int R) { return std::min((int64_t)b->B * ((per + R - 1) / R), (int64_t)b->rows * G / R + b->B); };
@@ -1045,7 +1047,7 @@ static Shape attend_shape(const spec_paged_cache *c, int cached_bytes, const spe
   s.R = 16 * s.qt;
   s.align = s.qt < 8 ? 128 : s.R * 64 / c->head_dim;
   s.tiles = tiles(s.R);
-  s.slots = std::max(1, 256 * attend_resident((int)dtype_bytes(c->dtype), cached_bytes, c->head_dim, s.qt) / (int)Hk);
+  s.slots = std::max(1, 256 * attend_resident((int)dtype_bytes(c->dtype), c->head_dim, s.qt) / (int)Hk);
   // What a tile can need at most decides whether any is cut, and so whether there is a second kernel, which costs a launch and the search for its work
   // even where it finds nothing to join.  us without cutting and with it, bf16, heads of 128.  One row of 64 sequences, 32 heads over 8: up to 1536 positions
   // 67 and 77, up to 4096 164 and 174; of one sequence: 768 positions 11 and 11, 1536 18 and 12, 4096 43 and 16.  So many sequences pay 5 to 20 %
@@ -1063,13 +1065,13 @@ static size_t attend_bytes(const spec_paged_cache *c, const Shape &s) {
   return (size_t)s.parts * c->n_kv_heads * s.R * (c->head_dim + 2) * sizeof(float);
 }
 // (behind paged_args)
-static int attend_check(const char *who, const spec_paged_cache *c, int cached_bytes, const spec_paged_batch *b, int n_q, int window, AttendArgs &a, Shape &s) {
+static int attend_check(const char *who, const spec_paged_cache *c, const spec_paged_batch *b, int n_q, int window, AttendArgs &a, Shape &s) {
   if (n_q < 1 || n_q % c->n_kv_heads)
     return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: n_q_heads=%d is not a multiple of n_kv_heads=%d", who, n_q, c->n_kv_heads);
   a.G = n_q / c->n_kv_heads;
   if ((int64_t)b->rows * a.G >= 1 << 30) return fail_noctx(SPEC_ERR_CAPACITY, "%s: more than 2^30 query rows of a key head", who);
   if (b->B == 0 || b->rows == 0) { s = Shape{};  return SPEC_OK; }
-  s = attend_shape(c, cached_bytes, b, n_q, window);
+  s = attend_shape(c, b, n_q, window);
   if (s.units * c->n_kv_heads * 512 >= (int64_t)1 << 32)
     return fail_noctx(SPEC_ERR_CAPACITY, "%s: %lld tiles of %d key heads are beyond one launch", who, (long long)s.units, c->n_kv_heads);
   return SPEC_OK;
@@ -1100,22 +1102,20 @@ static void attend_launch(const AttendArgs &a, const Shape &s, hipStream_t st) {
   const dim3 grid((unsigned)(sizeof(S) == 1 && QT < 8 ? (groups + 63) / 64 * 64 : groups));
   if constexpr (QT >= 8) hipLaunchKernelGGL((k_paged_chunk<T, S, HD, QT / 2>), grid, dim3(32 * QT), pc_lds(QT / 2), st, a);
   else hipLaunchKernelGGL((k_paged_attend<T, S, HD, QT>), grid, dim3(256), 0, st, a);
-  if constexpr (sizeof(S) == 1 && QT < 8) {
-    if (s.cut) hipLaunchKernelGGL((k_paged_join_rows<T, HD, QT>), dim3((unsigned)(s.cut * a.p.n_kv_heads * 4 * QT)), dim3(256), 0, st, a, s.align);
-    return;
-  }
-  if (s.cut) hipLaunchKernelGGL((k_paged_join<T, HD, QT>), dim3((unsigned)(s.cut * a.p.n_kv_heads * QT)), dim3(256), 0, st, a, s.align);
+  if (!s.cut) return;
+  if constexpr (sizeof(S) == 1 && QT < 8)
+    hipLaunchKernelGGL((k_paged_join_rows<T, HD, QT>), dim3((unsigned)(s.cut * a.p.n_kv_heads * 4 * QT)), dim3(256), 0, st, a, s.align);
+  else hipLaunchKernelGGL((k_paged_join<T, HD, QT>), dim3((unsigned)(s.cut * a.p.n_kv_heads * QT)), dim3(256), 0, st, a, s.align);
 }
 
-
 // A call: checked, with its arguments in `a` and its shape in `s`, behind paged_args.  nothing: there is no work.
-static int attend_prepare(const char *who, const spec_paged_cache *cache, int cached_bytes, const spec_paged_batch *batch, int n_q_heads, const void *d_q,
+static int attend_prepare(const char *who, const spec_paged_cache *cache, const spec_paged_batch *batch, int n_q_heads, const void *d_q,
                           int64_t q_stride, float scale, int window, void *d_workspace, size_t workspace_bytes, void *d_out, int64_t out_stride,
                           AttendArgs &a, Shape &s, bool &nothing) {
   // A window that reaches over all positions is none.  (So a window is at most 2^30, and its differences with positions stay inside 32 bits, those
   // of dead rows as well.)
   const bool endless = window >= batch->max_len;
-  int rc = attend_check(who, cache, cached_bytes, batch, n_q_heads, endless ? 0 : std::max(window, 0), a, s);
+  int rc = attend_check(who, cache, batch, n_q_heads, endless ? 0 : std::max(window, 0), a, s);
   if (rc) return rc;
   a.sl2 = scale * 1.4426950408889634f;
   if (!(scale > 0.f) || std::isinf(a.sl2)) return fail_noctx(SPEC_ERR_INVALID_ARG, "%s: scale must be positive and below 2.3e38", who);
