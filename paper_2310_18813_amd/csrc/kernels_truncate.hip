@@ -524,8 +524,8 @@ __global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
     }
     // One pass over what is looked at a turn, until it is few tokens: list it where there is room; else its bounds, and which of 256 parts between
     // them has the border.  (Eight bits of at most 64 every two turns, for two borders: the limit is never met.)
-    enum { LIST, BOUNDS, PARTS, SUM, LAST };
-    bool bounded = true, summing = false;
+    enum { LIST, BOUNDS, PARTS, LAST };
+    bool bounded = true;
     int drop = 0;
     u64 base = place_of(sc.zero, 0);
     // Parts from the first bin on: they need not end where the bins do.
@@ -540,7 +540,7 @@ __global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
     parts_of_bins();
 #pragma unroll 1
     for (int turn = 0; searching && turn < 48; ++turn) {
-      const int mode = summing ? SUM : !from_list && n <= Sh::LIST ? LIST : from_list && n <= TR_LAST ? LAST : bounded ? PARTS : BOUNDS;
+      const int mode = !from_list && n <= Sh::LIST ? LIST : from_list && n <= TR_LAST ? LAST : bounded ? PARTS : BOUNDS;
       __syncthreads();
       if (threadIdx.x == 0) {
         if (mode == LIST) sh.listed = 0;
@@ -549,19 +549,15 @@ __global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
       if (mode == PARTS)
         for (int i = threadIdx.x; i < TR_FINE; i += NT) { sh.fine_mass[i] = 0; sh.fine_cnt[i] = 0; }
       __syncthreads();
-      u64 least = ~0ull, most = 0, sum = 0;
+      u64 least = ~0ull, most = 0;
       auto take = [&](u64 at, float z) {  // (lists and orders are below: a wave counts its tokens first, since a thousand additions to one word of LDS take 10 us)
         if (at < lo || at > hi) return;
         if (mode == BOUNDS) {
           least = min(least, at); most = max(most, at);
         } else {
-          const u64 w = wt.number(z);
-          sum += w;
-          if (mode == PARTS) {
-            const int part = (int)min((u64)(TR_FINE - 1), (at - min(at, base)) >> drop);
-            atomicAdd(&sh.fine_cnt[part], 1u);
-            atomicAdd(&sh.fine_mass[part], w);
-          }
+          const int part = (int)min((u64)(TR_FINE - 1), (at - min(at, base)) >> drop);
+          atomicAdd(&sh.fine_cnt[part], 1u);
+          atomicAdd(&sh.fine_mass[part], wt.number(z));
         }
       };
       if (from_list) {
@@ -703,12 +699,6 @@ __global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
         if (part > 0) lo = max(lo, begin);
         if (part < TR_FINE - 1) hi = min(hi, begin + ((1ull << drop) - 1));
         bounded = false;
-      } else if (mode == SUM) {
-        uint32_t c = 0;
-        scan<NT>(sh, c, sum, all_c, all_m);
-        target = part_of(all_m);
-        bc = 0; bm = 0; n = min((uint32_t)k, n);
-        summing = false;
       } else {
         // Few tokens: four threads each, which add up those of a quarter of them that come up to it.  (Their sums go where none of the others' is read.)
         if (threadIdx.x == 0) sh.found_place = ~0ull;
@@ -743,19 +733,29 @@ __global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
         }
         __syncthreads();
         border = sh.found_place;
-        searching = r.by_p && !by_mass && border != ~0ull;
-        by_mass = true;
-        if (searching && r.few) {
-          lo = 0; hi = border;  // of the first k the sum, and its part
-          n = (uint32_t)k;
-          from_list = from_list && all_listed;
-          base = place_of(sc.zero, 0);
-          parts_to(border);
-          summing = true;
-        } else if (searching) {
-          target = part_of(sh.found_mass);  // (reached among the first k at the latest: the bins need not know of them)
-          searching = look_at_bin();
-          parts_of_bins();
+        searching = false;
+        if (r.by_p && !by_mass && border != ~0ull) {  // of the first k their sum, and its part, which is reached among them at the latest
+          by_mass = true;
+          target = part_of(sh.found_mass);
+          if (target > bm) {  // among these tokens, whose sums are there
+            __syncthreads();  // (all have read the first border)
+            if ((int)threadIdx.x < some) {
+              const u64 m = sh.last_mass[threadIdx.x];
+              if (m >= target && m - sh.fine_mass[TR_LAST + threadIdx.x] < target) sh.found_place = sh.fine_mass[threadIdx.x];
+            }
+            __syncthreads();
+            border = sh.found_place;
+          } else if (r.few) {
+            lo = 0; hi = border; bc = 0; bm = 0;
+            n = (uint32_t)k;
+            from_list = from_list && all_listed;
+            base = place_of(sc.zero, 0);
+            parts_to(border);
+            searching = true;
+          } else {  // (the bins need not know of the first k)
+            searching = look_at_bin();
+            parts_of_bins();
+          }
         }
       }
     }
