@@ -110,6 +110,48 @@ def test_long_contexts_are_cut_and_joined(B, td):
     run(B, td, 16, 1, 128, 64, [9, 1, 30], [6000, 4000, 2000])
 
 
+@pytest.mark.parametrize("Hq,Hk,hd", [(16, 8, 64), (16, 16, 128), (24, 24, 64), (32, 8, 128)])
+def test_heads_in_groups_of_eight(B, Hq, Hk, hd):
+    """Heads of one unit of work that run side by side: short, of many sequences, and cut into chunks."""
+    run(B, torch.bfloat16, Hq, Hk, hd, 16, [1, 3, 0, 2], [1, 70, 5, 300], absent=((3, 2),))
+    run(B, torch.float16, Hq, Hk, hd, 16, [1, 1], [3500, 40])
+
+
+@pytest.mark.parametrize("Hk", [2, 8])
+def test_more_than_64_sequences(B, Hk):
+    g = torch.Generator().manual_seed(21)
+    lens = torch.randint(0, 90, (131,), generator=g).tolist()
+    run(B, torch.bfloat16, 2 * Hk, Hk, 64, 16, torch.randint(0, 4, (131,), generator=g).tolist(), lens)
+    lens[77] = 2500
+    run(B, torch.float16, 2 * Hk, Hk, 64, 16, [1] * 131, lens, ragged=False)
+
+
+@pytest.mark.parametrize("td", TYPES)
+def test_a_pool_beyond_4_gigabytes(B, td):
+    """The last pages of pools of 5 GB: what small pools give."""
+    Hk, hd, page = 8, 128, 16
+    n = 5 * (1 << 30) // (page * Hk * hd)
+    b = ref.Batch([2, 2], [50, 20], page, ragged=False)
+    freq = B.spec_rope_frequencies(10000.0, hd)
+    t = B.HeadTransform(freq)
+    q, k, v = (b.heads(h, hd, td).to(DEV) for h in (16, Hk, Hk))
+    small, batch = B.PagedCache8.empty(b.n_pages, page, Hk, hd, td), b.on_gpu(B)
+    codes = [torch.empty((n, page, Hk, hd), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    scales = [torch.empty((n, Hk, page), dtype=torch.uint8, device=DEV) for _ in range(2)]
+    for c, sc in zip(codes, scales):
+        c[n - b.n_pages:] = 0
+        sc[n - b.n_pages:] = 127
+    large = B.PagedCache8(*codes, *scales, td)
+    far = B.PagedBatch(torch.where(batch.pages >= 0, batch.pages + (n - b.n_pages), -1).to(torch.int32), batch.lengths, b.T)
+    for other, (cache, bt) in enumerate(((small, batch), (large, far))):
+        got = B.spec_paged8_append(cache, bt, q, k, v, t)
+        back = B.spec_paged8_read(cache, bt)
+        o = B.spec_paged8_attention(cache, bt, got)
+        if not other:
+            want = (got, *back, o)
+    assert all(torch.equal(x, y) for x, y in zip((got, *back, o), want)) and want[3].isfinite().all() and want[1].any()
+
+
 @pytest.mark.parametrize("td", TYPES)
 @pytest.mark.parametrize("hd,rows", [(64, 3), (128, 3), (128, 20), (64, 70), (128, 140)])
 def test_nan_at_positions_that_some_rows_see(B, td, hd, rows):

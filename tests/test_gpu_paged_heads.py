@@ -123,6 +123,14 @@ def test_append_of_8_bits_and_back(B, shape, rows, lens, ragged, absent):
     assert (ksc.transpose(1, 2)[~owned] == mark).all() and (vsc.transpose(1, 2)[~owned] == mark).all()
 
 
+def test_more_than_64_sequences(B):
+    g = torch.Generator().manual_seed(22)
+    rows, lens = torch.randint(0, 3, (150,), generator=g).tolist(), torch.randint(0, 60, (150,), generator=g).tolist()
+    test_append_of_8_bits_and_back(B, SHAPES[1], rows, lens, True, ())
+    test_append_of_8_bits_and_back(B, SHAPES[3], [1] * 150, lens, False, ())
+    test_normed_append(B, SHAPES[0], rows, lens, True, ())
+
+
 def one_row(B, td, x, hd):
     """x [heads][hd] as the values of one position of a cache of 8 bits -> (codes, scale bytes, what is read back), on the CPU."""
     Hk = x.shape[0]

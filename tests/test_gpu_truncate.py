@@ -146,6 +146,18 @@ def test_narrow_and_wide_rows(B):
     run(B, steep.to(DEV), top_k=[6000, 6000], top_p=[1.0, 0.999])
 
 
+def test_the_border_of_flat_rows_wherever_their_logits_lie(B):
+    """More tokens in front of the border than a list holds: around zero, far from it on either side, and as differences of tiny or of huge numbers."""
+    V, g = 40003, torch.Generator().manual_seed(23)
+    shift = torch.tensor([0.0, 3.0, -3.0, 200.0, -200.0, 0.0, 0.0, 0.0])
+    size = torch.tensor([1.0, 1.0, 1.0, 0.5, 0.5, 1e-30, 1e30, 1e-42])
+    z = shift[:, None, None] + size[:, None, None] * torch.randn((8, 1, V), generator=g)
+    z[2] = z[2].clamp(max=0.0)  # the largest logit is zero, and many are
+    T = [1.0, 0.9, 1.1, 1.0, 1.0, 1e-30, 1e30, 1e-42]
+    run(B, z.to(DEV), temperature=T, top_p=[0.9] * 8)
+    run(B, z.to(DEV), temperature=T, top_k=[20000, 9000, 30000, 20000, 20000, 20000, 20000, 20000], top_p=[1.0, 0.95, 0.9, 0.5, 1.0, 1.0, 1.0, 1.0])
+
+
 def test_infinities_nan_and_masked_rows(B):
     V, inf = 3001, math.inf
     z = logits_of(8, 1, V, seed=8).cpu()
