@@ -970,8 +970,9 @@ __global__ __launch_bounds__(256) void k_paged_join(AttendArgs a, int align) {
   for (int d = 0; d < VE; ++d) Conv<T>::st(dst, d, none ? 0.f : o[d] * inv);
 }
 
-// The same with a wave a query row, whose four quarters take every fourth chunk: for a few rows that are cut into many chunks, which 16 lanes join one
-// after the other.  One row of 32 heads over 8, fp16, 32000 positions in 63 chunks of 8 bits: the join 22 -> 9 us, the call 38.1 -> 24.7.
+// The same with a wave a query row: a lane a chunk for maxima and sums, then a quarter every fourth chunk for the elements.  For a few rows that are cut
+// into many chunks, which 16 lanes join one after the other: one row of 32 heads over 8, fp16, 32000 positions in 63 chunks of 8 bits, the call 38.1 us
+// with 16 lanes a row, 24.7 with running maxima in every quarter, 21.2 so.
 template <class T, int HD, int QT>
 __global__ __launch_bounds__(256) void k_paged_join_rows(AttendArgs a, int align) {
   constexpr int R = 16 * QT, VE = HD / 16, AHEAD = 8;
@@ -980,7 +981,7 @@ __global__ __launch_bounds__(256) void k_paged_join_rows(AttendArgs a, int align
   if (!find_work<true>(a, R, align, unit, w)) return;
   w = in_scalars(w);
   const PagedSeq s = w.s;
-  const int row = blockIdx.x % (R / 4) * 4 + (threadIdx.x >> 6), quarter = threadIdx.x >> 4 & 3, d0 = VE * (threadIdx.x & 15), f = w.tile * R + row;
+  const int lane = threadIdx.x & 63, row = blockIdx.x % (R / 4) * 4 + (threadIdx.x >> 6), quarter = lane >> 4, d0 = VE * (lane & 15), f = w.tile * R + row;
   if (f >= s.n * a.G) return;
   const int64_t next = (int64_t)((s.n * a.G + R - 1) / R) * Hk * R, at = ((int64_t)w.part * Hk + hk) * R + row;
   const float2 *ml = (const float2 *)a.ml + at;
@@ -988,35 +989,37 @@ __global__ __launch_bounds__(256) void k_paged_join_rows(AttendArgs a, int align
   float m = -INFINITY, l = 0.f, o[VE];
 #pragma unroll
   for (int d = 0; d < VE; ++d) o[d] = 0.f;
-  for (int c0 = quarter; c0 < w.chunks; c0 += 4 * AHEAD) {
-    float2 x[AHEAD];
-    f32x4_v y[AHEAD][VE / 4];
+  for (int c0 = 0; c0 < w.chunks; c0 += 64) {
+    const bool on = c0 + lane < w.chunks;
+    const float2 x = ml[min(c0 + lane, w.chunks - 1) * next];
+    float wt = 0.f;
+    for (int j0 = 0; j0 < min(64, w.chunks - c0); j0 += 4 * AHEAD) {
+      f32x4_v y[AHEAD][VE / 4];
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      const int64_t c = min(c0 + 4 * i, w.chunks - 1) * next;
-      x[i] = ml[c];
+      for (int i = 0; i < AHEAD; ++i)
 #pragma unroll
-      for (int d = 0; d < VE / 4; ++d) y[i][d] = *(const f32x4_v *)(part + c * HD + 4 * d);
-    }
+        for (int d = 0; d < VE / 4; ++d) y[i][d] = *(const f32x4_v *)(part + min(c0 + j0 + 4 * i + quarter, w.chunks - 1) * next * HD + 4 * d);
+      if (j0 == 0) {  // (behind the first loads)
+        const float mn = fmaxf(m, wave_max(on ? x.x : -INFINITY)), was = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * a.sl2);
+        wt = !on || x.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x.x - mn) * a.sl2);
+        m = mn;
+        l = l * was + wave_sum(on ? x.y * wt : 0.f);
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      if (c0 + 4 * i >= w.chunks) break;
-      const float mn = fmaxf(m, x[i].x);
-      const float was = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * a.sl2), wt = x[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((x[i].x - mn) * a.sl2);
-      m = mn;
-      l = l * was + x[i].y * wt;
+        for (int d = 0; d < VE; ++d) o[d] *= was;
+      }
 #pragma unroll
-      for (int d = 0; d < VE; ++d) o[d] = o[d] * was + y[i][d / 4][d % 4] * wt;
+      for (int i = 0; i < AHEAD; ++i) {
+        const int j = j0 + 4 * i + quarter;
+        const float wj = __shfl(wt, j, 64);
+#pragma unroll
+        for (int d = 0; d < VE; ++d) o[d] += c0 + j < w.chunks ? y[i][d / 4][d % 4] * wj : 0.f;
+      }
     }
   }
 #pragma unroll
   for (int other = 16; other <= 32; other <<= 1) {
-    const float mo = __shfl_xor(m, other, 64), lo = __shfl_xor(l, other, 64), mn = fmaxf(m, mo);
-    const float own = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mn) * a.sl2), wt = mo == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mo - mn) * a.sl2);
-    m = mn;
-    l = l * own + lo * wt;
 #pragma unroll
-    for (int d = 0; d < VE; ++d) o[d] = o[d] * own + __shfl_xor(o[d], other, 64) * wt;
+    for (int d = 0; d < VE; ++d) o[d] += __shfl_xor(o[d], other, 64);
   }
   if (quarter) return;
   const bool none = nothing_seen(m, l);

@@ -108,6 +108,8 @@ def test_long_contexts_are_cut_and_joined(B, td):
     run(B, td, 8, 2, 128, 64, [1], [9000])
     run(B, td, 4, 1, 64, 16, [3, 1], [5000, 2600], window=3000)
     run(B, td, 16, 1, 128, 64, [9, 1, 30], [6000, 4000, 2000])
+    run(B, td, 4, 1, 128, 128, [1, 1], [20001, 17])  # more chunks than lanes
+    run(B, td, 4, 1, 64, 64, [4], [9000], absent=((0, 3), (0, 140)))
 
 
 @pytest.mark.parametrize("Hq,Hk,hd", [(16, 8, 64), (16, 16, 128), (24, 24, 64), (32, 8, 128)])
