@@ -16,8 +16,8 @@
 //                   its limit.  What the maxima rule out is not read.  Draws, where all that is kept is in the list.
 //   k_row_finish    the result; logits that the maxima rule out are not read.  Sums of the kept weights by 256 tokens, for
 //   k_row_draw      the other rows' draws.
-// 64 x 4 rows of 50272 bf16 logits, each sequence with its own rules: 9.6 + 15.4 + 34 + 16 + 4.6 us of 77; 24 x 8 fp32 rows of 151936: 28 + 16 + 52 + 28 + 5 of
-// 128; one row of 32000: 23.  The maxima and the result are at memory's rate (a copy's); the border is a chain of passes, 1.5 to 3 us
+// 64 x 4 rows of 50272 bf16 logits, each sequence with its own rules: 9 + 14 + 33 + 16 + 4.6 us of 76; 24 x 8 fp32 rows of 151936: 28 + 15 + 44 + 28 + 5 of
+// 120; one row of 32000: 21, greedy 10.  The maxima and the result are at memory's rate (a copy's); the border is a chain of passes, 1.5 to 3 us
 // each from the list, and of trips to L2 where it reads the row: a workgroup a row, those whose border lies among all tokens last.  A
 // workgroup for all of a row took 113, 297 and 45: rows that need all their weights kept their CU while others had nothing to do.
 // What cost most in LDS: additions that return a place in a list, all to one word (3000 of them 30 us), so that a wave counts its tokens first.
