@@ -4,8 +4,10 @@
 // kept.  A token's place in the order is one number of 64 bits, its logit's bits turned round over its id.
 //
 // Whether a sum of weights reaches top_p of the total decides which token is the last, and it has to be the same whatever order the sum
-// was taken in.  So weights are whole numbers, e^x times a power of two to nearest, and sums of them are exact: 2^50 for
-// a weight of 1 up to 4096 tokens, 2^44 with 151936.  Their exponential is computed in 64 bits (a power of two times a polynomial of degree 10 on half an octave).
+// was taken in.  So weights are whole numbers of a unit and sums of them are exact.  One unit for all would leave the many small weights of a long tail few
+// bits, and errors of equal weights add up (a tail of 151935 tokens of e^-25 in units of 2^-44: 89 tokens too few of 83266).  So a weight is a whole number of up to
+// 2^shift times the unit of its octave, 2^-(shift + octave); the sum of a bin, which lies within an octave, is 64 bits, other sums are two of 64 bits in the last
+// octave's unit.  Shift is 50 up to 4096 tokens, 44 with 151936.  The exponential is computed in 64 bits (a power of two times a polynomial of degree 10 on half an octave).
 //
 // Rows differ in what they ask for, and a row has more work than a compute unit does quickly, so that all but the search for the border
 // is cut into pieces of rows:
@@ -30,7 +32,7 @@ namespace spec {
 
 typedef unsigned long long u64;
 
-constexpr int TR_BINS = 2048, TR_PER_OCTAVE = 64;  // bins of weights: 32 octaves of them
+constexpr int TR_BINS = 2048, TR_PER_OCTAVE = 64, TR_OCTAVES = TR_BINS / TR_PER_OCTAVE;  // bins of weights; the last octave has all smaller ones
 constexpr int TR_FINE = 256;   // parts that what is looked at is cut into
 constexpr int TR_LAST = 128;   // tokens that are put in order at once
 constexpr int TR_FEW = 1024;   // the largest top-k that goes by the maxima alone
@@ -38,6 +40,26 @@ constexpr int TR_PIECES = 64;  // of a row, for its maxima
 // Pieces that a row with bins is cut into, at most: more fill the chip, but one workgroup reads the bins of all (16 KB each, some 0.3 us).  8, 12, 16 and 37
 // pieces, us: one row of 151936 with top-p 54.9, 53.7, 53.7, 56.7; 8 of them 55.6, 54.7, 54.5, 60.8; 32 with a top-k of 30000 79.6, 83.4, 83.6, 86.7.
 constexpr int TR_CUTS = 8;
+
+// A whole number of up to 94 bits: its lower 36 bits and those above, which are added up apart (2^28 of each fit); `plain` carries.
+struct Sum {
+  static constexpr int LOW = 36;
+  static constexpr u64 MASK = (1ull << LOW) - 1;
+  u64 lo, hi;
+  __device__ __forceinline__ Sum operator+(const Sum &o) const { return Sum{lo + o.lo, hi + o.hi}; }
+  __device__ __forceinline__ Sum operator-(const Sum &o) const { return Sum{lo - o.lo, hi - o.hi}; }  // (of a part of the same terms)
+  __device__ __forceinline__ Sum plain() const { return Sum{lo & MASK, hi + (lo >> LOW)}; }
+  __device__ __forceinline__ double about() const { return (double)hi * (MASK + 1) + (double)lo; }
+  static __device__ __forceinline__ Sum whole(double v) {  // of one from 0 on, below 2^94
+    const u64 hi = (u64)(v * (1. / (MASK + 1)));
+    return Sum{(u64)(v - (double)hi * (MASK + 1)), hi};
+  }
+};
+// as numbers; b: plain
+__device__ __forceinline__ bool less(const Sum &a, const Sum &b) {
+  const Sum x = a.plain();
+  return x.hi < b.hi || (x.hi == b.hi && x.lo < b.lo);
+}
 
 // What is found out about a row: kept is a logit that is larger than last_z, or equal with an id up to last_id; x = (z - zero) / temp.
 struct RowBorder {
@@ -50,7 +72,7 @@ struct RowBorder {
 struct TruncateArgs {
   const void *logits;
   int64_t row_stride;
-  int row0, q, V, shift;  // first row of the launch; rows of a sequence; a weight of 1 is 2^shift
+  int row0, q, V, shift;  // first row of the launch; rows of a sequence; bits of a weight
   const float *temperature;
   const int32_t *top_k;
   const float *top_p, *min_p;
@@ -60,7 +82,8 @@ struct TruncateArgs {
   // workspace
   float *piece_max, *max16;   // [rows][TR_PIECES], [rows][n16]
   RowBorder *border;          // [rows]
-  u64 *sums, *masses;         // [rows][stretches], [rows][cuts][TR_BINS]
+  Sum *sums;                  // [rows][stretches]
+  u64 *masses;                // [rows][cuts][TR_BINS]
   uint32_t *counts;           // [rows][cuts][TR_BINS]
   int pieces, piece;          // pieces of a row and tokens of one (a multiple of 1024), for the maxima
   int cuts, cut, B;           // for the masses; sequences
@@ -95,13 +118,18 @@ __device__ __forceinline__ float of_rank(uint32_t up) { return __uint_as_float(u
 __device__ __forceinline__ u64 place_of(float z, int id) { return (u64)~rank_of(z + 0.f) << 32 | (uint32_t)id; }
 __device__ __forceinline__ float logit_of(u64 place) { return of_rank(~(uint32_t)(place >> 32)); }
 
-// A row's weights: log2 of one, and itself as a whole number.
+// A row's weights: log2 of one, its bin and octave, and itself as a whole number.
 struct Weights {
   double M, c;  // largest logit, log2(e) / temperature
   int shift;
   __device__ __forceinline__ double log2_of(float z) const { return fmax(((double)z - M) * c, -1100.); }  // (-infinity at any temperature as well)
-  __device__ __forceinline__ u64 number(float z) const {
-    const double y = log2_of(z), n = rint(y), f = y - n;
+  // y: a log2, up to 0.  Bins never fall as logits do.
+  static __device__ __forceinline__ int bin(double y) { return min((int)(y * -TR_PER_OCTAVE), TR_BINS - 1); }
+  static __device__ __forceinline__ int octave_of(int bin) { return (int)((uint32_t)bin / TR_PER_OCTAVE); }
+  static __device__ __forceinline__ int octave(double y) { return min((int)-y, TR_OCTAVES - 1); }  // octave_of(bin(y))
+  // in units of the octave's own
+  __device__ __forceinline__ u64 number(double y, int octave) const {
+    const double n = rint(y), f = y - n;
     // the Taylor series of 2^f: what is left out is below (ln 2 / 2)^11 / 11! = 2.2e-13 of it
     double p = 7.0549116208011233e-9;
     p = fma(p, f, 1.0178086009239699e-7);
@@ -114,8 +142,16 @@ struct Weights {
     p = fma(p, f, 0.24022650695910071);
     p = fma(p, f, 0.69314718055994531);
     p = fma(p, f, 1.);
-    const double v = ldexp(p, (int)n + shift) + 4503599627370496.;  // 2^52: the sum's bits are the number, to nearest
+    const double v = ldexp(p, (int)n + octave + shift) + 4503599627370496.;  // 2^52: the sum's bits are the number, to nearest
     return __builtin_bit_cast(u64, v) & 0xfffffffffffffull;
+  }
+  // in units of the last octave's
+  static __device__ __forceinline__ Sum in_last(u64 r, int octave) {
+    return Sum{r << (TR_OCTAVES - 1 - octave) & Sum::MASK, r >> (Sum::LOW - TR_OCTAVES + 1 + octave)};
+  }
+  __device__ __forceinline__ Sum number(float z) const {
+    const double y = log2_of(z);
+    return in_last(number(y, octave(y)), octave(y));
   }
 };
 
@@ -141,7 +177,7 @@ struct RowScale {
   float top, zero;  // the largest logit; 0 where it is infinite: then infinite ones share the weight and the others have none, and 0 and -infinity stand for them
   bool endless;
   Weights wt;
-  float per_unit;
+  float per_unit;  // bins, about, to a logit
   __device__ __forceinline__ RowScale(const TruncateArgs &a, int row, float temp) {
     const int lane = threadIdx.x & 63;
     top = wave_max(a.piece_max[(int64_t)row * TR_PIECES + min(lane, a.pieces - 1)]);
@@ -151,8 +187,7 @@ struct RowScale {
     per_unit = fminf((float)(wt.c * TR_PER_OCTAVE), 3e38f);
   }
   __device__ __forceinline__ float of(float z) const { return !endless ? z : z == INFINITY ? 0.f : -INFINITY; }
-  // A token's bin, which never falls as its logit falls.  (0 times infinity would be the last one's.)
-  __device__ __forceinline__ int bin(float z) const { return (int)fminf((zero - z) * per_unit, (float)(TR_BINS - 1)); }
+  __device__ __forceinline__ int bin(float z) const { return Weights::bin(wt.log2_of(z)); }
   // The largest logit up to `zero` in a bin from `first` on.  The wave tries 64 at a time.
   __device__ __forceinline__ float largest_from(int first) const {
     uint32_t is = rank_of(-INFINITY), past = rank_of(zero) + 1;  // it is from `is` on and before `past`
@@ -168,9 +203,10 @@ struct RowScale {
 // What a workgroup of NT threads that looks for a border holds.
 template <int NT> struct Truncate {
   static constexpr int WAVES = NT / 64, LIST = NT == 256 ? 1024 : 4096;
-  u64 list[LIST], mass[TR_BINS], fine_mass[TR_FINE], last_mass[TR_LAST], wave_u[2][WAVES], found_mass, found_place;
+  Sum target, before, found_mass, wave_m[WAVES];  // target, before: of the search, here since a wave has no registers left for them
+  u64 list[LIST], mass[TR_BINS], fine_lo[TR_FINE], fine_hi[TR_FINE], last_lo[TR_LAST], last_hi[TR_LAST], wave_u[2][WAVES], found_place;
   uint32_t cnt[TR_BINS], fine_cnt[TR_FINE], wave_c[WAVES], found_bin, found_cnt, found_n, listed, few;
-  static constexpr int UNITS = TR_BINS / 2;  // sums of weights over stretches of the row, in the place of mass
+  static constexpr int UNITS = TR_BINS / 2;  // sums of weights over stretches of the row, in the place of mass: lower limbs and upper ones
 };
 
 // Sums and maxima over the lanes of a wave up to each lane (so that the last one has that of all), without a trip through LDS.
@@ -185,6 +221,7 @@ template <class V> __device__ __forceinline__ V sum_to_lane(V v) {
   v += shifted<0x142, 0xa>(v); v += shifted<0x143, 0xc>(v);
   return v;
 }
+__device__ __forceinline__ Sum sum_to_lane(const Sum &v) { return Sum{sum_to_lane(v.lo), sum_to_lane(v.hi)}; }
 __device__ __forceinline__ u64 max_to_lane(u64 v) {
   v = max(v, shifted<0x111, 0xf>(v)); v = max(v, shifted<0x112, 0xf>(v)); v = max(v, shifted<0x114, 0xf>(v)); v = max(v, shifted<0x118, 0xf>(v));
   v = max(v, shifted<0x142, 0xa>(v)); v = max(v, shifted<0x143, 0xc>(v));
@@ -193,56 +230,58 @@ __device__ __forceinline__ u64 max_to_lane(u64 v) {
 
 // The sums of counts and weights up to a thread's own, and of all.
 template <int NT, class Sh>
-__device__ __forceinline__ void scan(Sh &sh, uint32_t &c, u64 &m, uint32_t &all_c, u64 &all_m) {
+__device__ __forceinline__ void scan(Sh &sh, uint32_t &c, Sum &m, uint32_t &all_c, Sum &all_m) {
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   c = sum_to_lane(c);
   m = sum_to_lane(m);
   __syncthreads();
-  if (lane == 63) { sh.wave_c[wv] = c; sh.wave_u[0][wv] = m; }
+  if (lane == 63) { sh.wave_c[wv] = c; sh.wave_m[wv] = m; }
   __syncthreads();
-  all_c = 0; all_m = 0;
+  all_c = 0; all_m = Sum{0, 0};
 #pragma unroll
   for (int i = 0; i < NT / 64; ++i) {
-    if (i == wv) { c += all_c; m += all_m; }
-    all_c += sh.wave_c[i]; all_m += sh.wave_u[0][i];
+    if (i == wv) { c += all_c; m = m + all_m; }
+    all_c += sh.wave_c[i]; all_m = all_m + sh.wave_m[i];
   }
 }
 
-// Among N bins of counts and sums, the one in which `target` is reached, by sum or by count; what lies before it goes on top of what
-// is there in before_*.  Leaves the bin and its count; false if no bin reaches it.
-template <int NT, int N>
-__device__ __forceinline__ bool find_bin(Truncate<NT> &sh, const uint32_t *cnt, const u64 *mass, bool by_mass, u64 target, uint32_t &before_cnt,
-                                         u64 &before_mass, int &bin, uint32_t &n) {
+// Among N bins of counts cnt[i] and sums masses(i, number of bins), the one in which sh.target is reached, by sum or by count; what lies before it goes on top
+// of what is there in before_cnt and sh.before.  Leaves the bin and its count; false if no bin reaches it.
+template <int NT, int N, class F>
+__device__ __forceinline__ bool find_bin(Truncate<NT> &sh, const uint32_t *cnt, F masses, bool by_mass, uint32_t &before_cnt, int &bin, uint32_t &n) {
   constexpr int PER = (N + NT - 1) / NT;
   const int first = threadIdx.x * PER;
-  uint32_t c[PER];
-  u64 m[PER];
-  uint32_t sc = 0;
-  u64 sm = 0;
+  const bool on = first < N;
+  uint32_t c = 0;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const bool on = first + i < N;
-    c[i] = on ? cnt[first + i] : 0; m[i] = on ? mass[first + i] : 0;
-    sc += c[i]; sm += m[i];
-  }
-  uint32_t to_c = sc, all_c;
-  u64 to_m = sm, all_m;
+  for (int i = 0; i < PER; ++i) c += on ? cnt[first + i] : 0;
+  Sum m = masses(on ? first : 0, std::integral_constant<int, PER>());
+  if (!on) m = Sum{0, 0};
+  uint32_t to_c = c, all_c;
+  Sum to_m = m, all_m;
   __syncthreads();
   if (threadIdx.x == 0) sh.found_bin = ~0u;
   scan<NT>(sh, to_c, to_m, all_c, all_m);
-  to_c += before_cnt - sc; to_m += before_mass - sm;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const u64 was = by_mass ? to_m : to_c, is = was + (by_mass ? m[i] : c[i]);
-    if (was < target && is >= target) {
-      sh.found_bin = first + i; sh.found_cnt = to_c; sh.found_mass = to_m; sh.found_n = c[i];
+  to_c += before_cnt; to_m = to_m + sh.before;
+  const Sum target = sh.target;
+  auto short_of = [&](uint32_t c, const Sum &m) { return by_mass ? less(m, target) : c < (uint32_t)target.lo; };
+  if (!short_of(to_c, to_m) && short_of(to_c - c, to_m - m)) {
+    // from the last of the thread's bins back to the one that reaches it
+#pragma unroll 1
+    for (int i = first + PER - 1;; --i) {
+      const uint32_t own_c = cnt[i];
+      to_c -= own_c; to_m = to_m - masses(i, std::integral_constant<int, 1>());
+      if (short_of(to_c, to_m)) {
+        sh.found_bin = i; sh.found_cnt = to_c; sh.found_mass = to_m; sh.found_n = own_c;
+        break;
+      }
     }
-    to_c += c[i]; to_m += m[i];
   }
   __syncthreads();
   bin = (int)sh.found_bin;
   if (bin < 0) return false;
-  before_cnt = sh.found_cnt; before_mass = sh.found_mass; n = sh.found_n;
+  before_cnt = sh.found_cnt; n = sh.found_n;
+  if (threadIdx.x == 0) sh.before = sh.found_mass;
   return true;
 }
 
@@ -258,56 +297,61 @@ struct Kept {
 
 // What a draw needs of LDS (a workgroup that looked for a border has it).
 template <int NT> struct DrawShared {
-  u64 wave_u[2][NT / 64], found_mass;
+  Sum found_mass, wave_m[NT / 64];
   uint32_t wave_c[NT / 64], found_bin;
 };
 
-// The draw of a row: the first token with which the sum of the kept weights, in the order of ids, exceeds u times their total.  sums: of n stretches of
+// The draw of a row: the first token with which the sum of the kept weights, in the order of ids, exceeds u times their total.  sums(i): of n stretches of
 // per * 256 tokens.
-template <class T, bool VEC, int NT, class Sh>
-__device__ __forceinline__ void draw_token(Sh &sh, const TruncateArgs &a, int row, const RowScale &sc, const Kept &kept, const u64 *sums, int n, int per) {
+template <class T, bool VEC, int NT, class Sh, class F>
+__device__ __forceinline__ void draw_token(Sh &sh, const TruncateArgs &a, int row, const RowScale &sc, const Kept &kept, F sums, int n, int per) {
   const int lane = threadIdx.x & 63, each = (n + NT - 1) / NT, s0 = min(n, (int)threadIdx.x * each), s1 = min(n, s0 + each);
   const T *z_row = (const T *)a.logits + (int64_t)row * a.row_stride;
-  u64 own = 0, total;
-  for (int s = s0; s < s1; ++s) own += sums[s];
-  if (threadIdx.x == 0) { sh.found_bin = 0; sh.found_mass = 0; }
-  u64 to = own;
+  Sum own{0, 0}, total;
+  for (int s = s0; s < s1; ++s) own = own + sums(s);
+  if (threadIdx.x == 0) { sh.found_bin = 0; sh.found_mass = Sum{0, 0}; }
+  Sum to = own;
   uint32_t none = 0, no_c;
   scan<NT>(sh, none, to, no_c, total);
-  const double want = (double)a.u[row] * (double)total;
-  const u64 target = want > 0. ? min(total - 1, (u64)want) : 0;  // exceeded from target + 1 on
-  u64 at = to - own;
-  if (at <= target && to > target) {
+  // exceeded from `target` on
+  total = total.plain();
+  const double want = (double)a.u[row] * total.about();
+  Sum target = want > 0. ? Sum::whole(fmin(want, total.about())) : Sum{0, 0};
+  target = Sum{target.lo + 1, target.hi}.plain();
+  if (less(total, target)) target = total;
+  Sum at = to - own;
+  if (less(at, target) && !less(to, target)) {
     for (int s = s0; s < s1; ++s) {
-      const u64 next = at + sums[s];
-      if (next > target) { sh.found_bin = s; sh.found_mass = at; break; }
+      const Sum next = at + sums(s);
+      if (!less(next, target)) { sh.found_bin = s; sh.found_mass = at; break; }
       at = next;
     }
   }
   __syncthreads();
   if (threadIdx.x >= 64) return;
-  u64 before = sh.found_mass;
-  for (int s = (int)sh.found_bin * per; s < min(a.stretches, ((int)sh.found_bin + 1) * per) && before <= target; ++s) {
+  Sum before = sh.found_mass;
+  for (int s = (int)sh.found_bin * per; s < min(a.stretches, ((int)sh.found_bin + 1) * per) && less(before, target); ++s) {
     const int x = 256 * s + 4 * lane;
     Quad<T, VEC> v;
     float z[4];
     v.load(z_row, x, a.V);
     v.numbers(x, a.V, z);
-    u64 w[4], sum = 0;
+    Sum w[4], sum{0, 0};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       z[i] = sc.of(z[i]);
-      w[i] = kept(z[i], x + i) ? sc.wt.number(z[i]) : 0;
-      sum += w[i];
+      w[i] = kept(z[i], x + i) ? sc.wt.number(z[i]) : Sum{0, 0};
+      sum = sum + w[i];
     }
-    const u64 up_to = sum_to_lane(sum);
-    u64 c = before + up_to - sum;
+    const Sum up_to = sum_to_lane(sum);
+    Sum c = before + up_to - sum;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (c <= target && c + w[i] > target) a.tokens[row] = x + i;
-      c += w[i];
+      const Sum next = c + w[i];
+      if (less(c, target) && !less(next, target)) a.tokens[row] = x + i;
+      c = next;
     }
-    before += __shfl(up_to, 63, 64);
+    before = before + Sum{__shfl(up_to.lo, 63, 64), __shfl(up_to.hi, 63, 64)};
   }
 }
 
@@ -394,14 +438,18 @@ __global__ __launch_bounds__(512) void k_row_masses(TruncateArgs a) {
       float z[4];
       v[i].numbers(x0 + 2048 * i, end, z);
       u64 w[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = sc.wt.number(z[e] = sc.of(z[e]));
+      int at[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int at = sc.bin(z[e]);
+        const double y = sc.wt.log2_of(z[e] = sc.of(z[e]));
+        at[e] = Weights::bin(y);
+        w[e] = sc.wt.number(y, Weights::octave_of(at[e]));
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
         if (z[e] > -INFINITY) {
-          atomicAdd(&mass[at], w[e]);
-          if (r.by_k) atomicAdd(&cnt[at], 1u);
+          atomicAdd(&mass[at[e]], w[e]);
+          if (r.by_k) atomicAdd(&cnt[at[e]], 1u);
         }
       }
     }
@@ -415,8 +463,10 @@ __global__ __launch_bounds__(512) void k_row_masses(TruncateArgs a) {
 }
 
 // ------------------------------------------------------------------ the border
+// (256 threads: three workgroups a CU, 600 x 2 rows of 8000 112 us, with two 127; rows that are not loaded in fours need registers for two.  512 threads: LDS has
+// room for two workgroups, registers for one.)
 template <class T, bool VEC, int NT>
-__global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
+__global__ __launch_bounds__(NT, NT == 256 && VEC ? 3 : 2) void k_row_border(TruncateArgs a) {
   typedef Truncate<NT> Sh;
   __shared__ Sh sh;
   const int row = a.row0 + blockIdx.x, lane = threadIdx.x & 63, wv = threadIdx.x >> 6, V = a.V;
@@ -464,22 +514,36 @@ __global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
     if (a.tokens && threadIdx.x == 0) a.tokens[row] = (int)(uint32_t)border;
   } else if (r.by_k || r.by_p) {
     // What is looked at: the tokens of bins first .. last whose places lie in lo .. hi, n of them, of the row or of the list.  The border is the first of
-    // them with which the count, or by_mass the sum, on top of bc or bm, reaches `target`.
+    // them with which the count, or by_mass the sum, on top of bc or sh.before, reaches sh.target.  (n may be too small before they are listed or picked.)
     int first = 0, last = TR_BINS - 1;
-    u64 lo = 0, hi = ~0ull, bm = 0, all_m = 0, target = (u64)max(k, 1);
-    uint32_t n = 0, bc = 0, all_c = 0;
+    u64 lo = 0, hi = ~0ull;
+    uint32_t n = 0, bc = 0, listing = 0;  // listing: tokens that a list takes, where there is room
     bool by_mass = false, searching = true;
-    auto part_of = [&](u64 total) { return max((u64)1, min(total, (u64)ceil(fmax((double)r.p, 0.) * (double)total))); };
-    // The bin where the count or the sum reaches `target` is looked at; with those before it where there is room for all.
+    auto set = [&](Sum &x, const Sum &to) {  // (read behind the next barrier)
+      if (threadIdx.x == 0) x = to;
+    };
+    set(sh.target, Sum{(u64)max(k, 1), 0});
+    set(sh.before, Sum{0, 0});
+    auto part_of = [&](const Sum &all) {
+      const Sum total = all.plain(), part = Sum::whole(fmin(fmax(ceil((double)r.p * total.about()), 1.), total.about()));
+      return less(part, total) ? part : total;
+    };
+    auto of_bins = [&](int i, auto N) {  // (of one octave)
+      u64 m = 0;
+#pragma unroll
+      for (int j = 0; j < decltype(N)::value; ++j) m += sh.mass[i + j];
+      return Weights::in_last(m, Weights::octave_of(i));
+    };
+    auto of_part = [&](int i, auto) { return Sum{sh.fine_lo[i], sh.fine_hi[i]}; };
+    // The bin where the count or the sum reaches `target` is looked at; those before it are listed as well where there is room for all.
     auto look_at_bin = [&]() {
-      bc = 0; bm = 0; lo = 0; hi = ~0ull;
+      bc = 0; lo = 0; hi = ~0ull;
+      set(sh.before, Sum{0, 0});
       from_list = false;
-      const bool there = find_bin<NT, TR_BINS>(sh, sh.cnt, sh.mass, by_mass, target, bc, bm, last, n);
-      if (bc + n <= Sh::LIST) {
-        first = 0; n += bc; bc = 0; bm = 0;
-      } else {
-        first = last;
-      }
+      const bool there = find_bin<NT, TR_BINS>(sh, sh.cnt, of_bins, by_mass, bc, last, n);
+      const bool with_front = bc + n <= Sh::LIST;
+      first = with_front ? 0 : last;
+      listing = with_front ? bc + n : n;
       return there;
     };
     if (r.few) {
@@ -498,11 +562,12 @@ __global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
         }
       }
       __syncthreads();
-      if (!find_bin<NT, TR_BINS>(sh, sh.cnt, sh.mass, false, target, bc, bm, last, n)) last = TR_BINS - 1;
-      bc = 0; bm = 0; n = 0;
+      if (!find_bin<NT, TR_BINS>(sh, sh.cnt, of_bins, false, bc, last, n)) last = TR_BINS - 1;
+      bc = 0; n = listing = 0;
+      set(sh.before, Sum{0, 0});
     } else {
-      uint32_t c = 0;
-      u64 m = 0;
+      uint32_t c = 0, all_c;
+      Sum m{0, 0}, all_m;
       constexpr int PER = (TR_BINS + NT - 1) / NT;
       const Cuts cuts(a);
       const int64_t at = cuts.first(a, row) * TR_BINS + threadIdx.x;
@@ -521,13 +586,13 @@ __global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
         const int of = threadIdx.x + i * NT;
         if (of >= TR_BINS) break;
         // A bin's weights are alike, so that its sum tells how many there are, a little high (the last one's, which may be small, aside).
-        if (!r.by_k) counts[i] = masses[i] ? 1 + (uint32_t)(ldexpf((float)masses[i], -a.shift) * exp2f((of + 1) * (1.01f / TR_PER_OCTAVE))) : 0;
+        if (!r.by_k) counts[i] = masses[i] ? 1 + (uint32_t)(ldexpf((float)masses[i], -a.shift) * exp2f((of % TR_PER_OCTAVE + 1) * (1.01f / TR_PER_OCTAVE))) : 0;
         sh.mass[of] = masses[i]; sh.cnt[of] = counts[i];
-        c += counts[i]; m += masses[i];
+        c += counts[i]; m = m + Weights::in_last(masses[i], Weights::octave_of(of));
       }
       scan<NT>(sh, c, m, all_c, all_m);
       by_mass = !(r.by_k && (uint32_t)k < all_c);
-      if (by_mass) target = part_of(all_m);
+      if (by_mass) set(sh.target, part_of(all_m));
       searching = (r.by_p || !by_mass) && look_at_bin();
     }
     // One pass over what is looked at a turn, until it is few tokens: list it where there is room; else its bounds, and which of 256 parts between
@@ -548,14 +613,14 @@ __global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
     parts_of_bins();
 #pragma unroll 1
     for (int turn = 0; searching && turn < 48; ++turn) {
-      const int mode = !from_list && n <= Sh::LIST ? LIST : from_list && n <= TR_LAST ? LAST : bounded ? PARTS : BOUNDS;
+      const int mode = !from_list && listing <= Sh::LIST ? LIST : from_list && n <= TR_LAST ? LAST : bounded ? PARTS : BOUNDS;
       __syncthreads();
       if (threadIdx.x == 0) {
         if (mode == LIST) sh.listed = 0;
         sh.few = 0;
       }
       if (mode == PARTS)
-        for (int i = threadIdx.x; i < TR_FINE; i += NT) { sh.fine_mass[i] = 0; sh.fine_cnt[i] = 0; }
+        for (int i = threadIdx.x; i < TR_FINE; i += NT) { sh.fine_lo[i] = 0; sh.fine_hi[i] = 0; sh.fine_cnt[i] = 0; }
       __syncthreads();
       u64 least = ~0ull, most = 0;
       auto take = [&](u64 at, float z) {  // (lists and orders are below: a wave counts its tokens first, since a thousand additions to one word of LDS take 10 us)
@@ -565,7 +630,11 @@ __global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
         } else {
           const int part = (int)min((u64)(TR_FINE - 1), (at - min(at, base)) >> drop);
           atomicAdd(&sh.fine_cnt[part], 1u);
-          atomicAdd(&sh.fine_mass[part], wt.number(z));
+          if (r.by_p) {
+            const Sum w = wt.number(z);
+            atomicAdd(&sh.fine_lo[part], w.lo);
+            if (w.hi) atomicAdd(&sh.fine_hi[part], w.hi);
+          }
         }
       };
       if (from_list) {
@@ -581,7 +650,10 @@ __global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
             uint32_t to = 0;
             if (lane == leader) to = atomicAdd(&sh.few, (uint32_t)__popcll(mask));
             to = __builtin_amdgcn_readlane(to, leader) + __popcll(mask & ((1ull << lane) - 1));
-            if (on && to < TR_LAST) { sh.fine_mass[to] = at; sh.fine_mass[TR_LAST + to] = wt.number(logit_of(at)); }
+            if (on && to < TR_LAST) {
+              const Sum w = wt.number(logit_of(at));
+              sh.fine_lo[to] = at; sh.fine_lo[TR_LAST + to] = w.lo; sh.fine_hi[to] = w.hi;
+            }
           } else {
             take(at, logit_of(at));
           }
@@ -684,11 +756,17 @@ __global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
       }
       __syncthreads();
       if (mode == LIST) {
-        n = sh.listed;
-        from_list = n <= Sh::LIST;
+        listing = sh.listed;
+        from_list = listing <= Sh::LIST;
         all_listed = lo == 0 && first == 0;
+        const bool in_front = !r.few && all_listed && last > 0;  // tokens that bc and sh.before count have been listed with the bin's own
+        if (!in_front || !from_list) n = listing;
+        if (in_front) {
+          lo = base = place_of(sc.largest_from(last), 0);
+          parts_to(max(base + 1, place_of(sc.zero - (float)(last + 2) / sc.per_unit, 0)));
+        }
         if (r.few && !by_mass && n <= (uint32_t)k && from_list && all_listed) {  // fewer finite ones than asked for, or just as many
-          target = n;
+          set(sh.target, Sum{n, 0});
           searching = n > 0;
         }
       } else if (mode == BOUNDS) {
@@ -703,60 +781,72 @@ __global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
         parts_to(hi);
       } else if (mode == PARTS) {
         int part;
-        searching = find_bin<NT, TR_FINE>(sh, sh.fine_cnt, sh.fine_mass, by_mass, target, bc, bm, part, n);
+        searching = find_bin<NT, TR_FINE>(sh, sh.fine_cnt, of_part, by_mass, bc, part, n);
         const u64 begin = base + ((u64)part << drop);
         if (part > 0) lo = max(lo, begin);
         if (part < TR_FINE - 1) hi = min(hi, begin + ((1ull << drop) - 1));
+        if (!from_list) listing = n;
         bounded = false;
+      } else if (sh.few > TR_LAST) {  // (a bin's number of tokens is known about)
+        n = sh.few;
       } else {
         // Few tokens: four threads each, which add up those of a quarter of them that come up to it.  (Their sums go where none of the others' is read.)
         if (threadIdx.x == 0) sh.found_place = ~0ull;
-        for (int i = threadIdx.x; i < TR_LAST; i += NT) { sh.fine_cnt[i] = bc; sh.last_mass[i] = bm; }
+        auto of_token = [&](int i) { return Sum{sh.fine_lo[TR_LAST + i], sh.fine_hi[i]}; };
+        auto up_to_token = [&](int i) { return Sum{sh.last_lo[i], sh.last_hi[i]}; };
+        for (int i = threadIdx.x; i < TR_LAST; i += NT) { sh.fine_cnt[i] = bc; sh.last_lo[i] = sh.before.lo; sh.last_hi[i] = sh.before.hi; }
         __syncthreads();
         const int some = (int)min(sh.few, (uint32_t)TR_LAST);
         for (int i = threadIdx.x; i < 4 * TR_LAST; i += NT) {
           const int of = i % TR_LAST, j0 = i / TR_LAST * (TR_LAST / 4);
           if (of >= some || j0 >= some) continue;
-          const u64 own = sh.fine_mass[of];
+          const u64 own = sh.fine_lo[of];
           uint32_t c = 0;
-          u64 m = 0;
+          u64 m_lo = 0, m_hi = 0;
 #pragma unroll 1
           for (int j = j0; j < min(some, j0 + TR_LAST / 4); j += 8) {
-            u64 other[8], w[8];
+            u64 other[8], lo8[8], hi8[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) { other[e] = sh.fine_mass[j + e]; w[e] = sh.fine_mass[TR_LAST + j + e]; }
+            for (int e = 0; e < 8; ++e) { other[e] = sh.fine_lo[j + e]; lo8[e] = sh.fine_lo[TR_LAST + j + e]; hi8[e] = sh.fine_hi[j + e]; }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const bool upto = j + e < some && other[e] <= own;
               c += upto;
-              m += upto ? w[e] : 0;
+              m_lo += upto ? lo8[e] : 0;
+              m_hi += upto ? hi8[e] : 0;
             }
           }
           atomicAdd(&sh.fine_cnt[of], c);
-          atomicAdd(&sh.last_mass[of], m);
+          atomicAdd(&sh.last_lo[of], m_lo);
+          atomicAdd(&sh.last_hi[of], m_hi);
         }
         __syncthreads();
         if ((int)threadIdx.x < some) {
-          const u64 m = sh.last_mass[threadIdx.x], to = by_mass ? m : sh.fine_cnt[threadIdx.x];
-          if (to >= target && to - (by_mass ? sh.fine_mass[TR_LAST + threadIdx.x] : 1) < target) { sh.found_place = sh.fine_mass[threadIdx.x]; sh.found_mass = m; }
+          const Sum m = up_to_token(threadIdx.x), target = sh.target;
+          if (by_mass ? !less(m, target) && less(m - of_token(threadIdx.x), target) : sh.fine_cnt[threadIdx.x] == (uint32_t)target.lo) {
+            sh.found_place = sh.fine_lo[threadIdx.x]; sh.found_mass = m;
+          }
         }
         __syncthreads();
         border = sh.found_place;
         searching = false;
         if (r.by_p && !by_mass && border != ~0ull) {  // of the first k their sum, and its part, which is reached among them at the latest
           by_mass = true;
-          target = part_of(sh.found_mass);
-          if (target > bm) {  // among these tokens, whose sums are there
-            __syncthreads();  // (all have read the first border)
+          const Sum target = part_of(sh.found_mass);
+          const bool among = less(sh.before, target);  // these tokens, whose sums are there
+          __syncthreads();  // (all have read the first border and what lies before it)
+          set(sh.target, target);
+          if (among) {
             if ((int)threadIdx.x < some) {
-              const u64 m = sh.last_mass[threadIdx.x];
-              if (m >= target && m - sh.fine_mass[TR_LAST + threadIdx.x] < target) sh.found_place = sh.fine_mass[threadIdx.x];
+              const Sum m = up_to_token(threadIdx.x);
+              if (!less(m, target) && less(m - of_token(threadIdx.x), target)) sh.found_place = sh.fine_lo[threadIdx.x];
             }
             __syncthreads();
             border = sh.found_place;
           } else if (r.few) {
-            lo = 0; hi = border; bc = 0; bm = 0;
-            n = (uint32_t)k;
+            lo = 0; hi = border; bc = 0;
+            set(sh.before, Sum{0, 0});
+            n = listing = (uint32_t)k;
             from_list = from_list && all_listed;
             base = place_of(sc.zero, 0);
             parts_to(border);
@@ -785,17 +875,21 @@ __global__ __launch_bounds__(NT) void k_row_border(TruncateArgs a) {
   if (threadIdx.x == 0) a.border[row] = RowBorder{wt.c, last_z, sc.zero, r.temp, last_id, sc.endless, draw || k == 1};
   if (!draw) return;
   __syncthreads();
-  for (int i = threadIdx.x; i < Sh::UNITS; i += NT) sh.mass[i] = 0;
+  for (int i = threadIdx.x; i < 2 * Sh::UNITS; i += NT) sh.mass[i] = 0;
   __syncthreads();
   const Kept kept{last_z, last_id};
   const int per = (a.stretches + Sh::UNITS - 1) / Sh::UNITS;
   for (uint32_t i = threadIdx.x; i < sh.listed; i += NT) {
     const u64 at = sh.list[i];
     const int id = (int)(uint32_t)at;
-    if (kept(logit_of(at), id)) atomicAdd(&sh.mass[(id >> 8) / per], wt.number(logit_of(at)));
+    if (kept(logit_of(at), id)) {
+      const Sum w = wt.number(logit_of(at));
+      atomicAdd(&sh.mass[(id >> 8) / per], w.lo);
+      if (w.hi) atomicAdd(&sh.mass[Sh::UNITS + (id >> 8) / per], w.hi);
+    }
   }
   __syncthreads();
-  draw_token<T, VEC, NT>(sh, a, row, sc, kept, sh.mass, Sh::UNITS, per);
+  draw_token<T, VEC, NT>(sh, a, row, sc, kept, [&](int i) { return Sum{sh.mass[i], sh.mass[Sh::UNITS + i]}; }, Sh::UNITS, per);
 }
 
 // ------------------------------------------------------------------ the result
@@ -822,27 +916,28 @@ __global__ __launch_bounds__(256) void k_row_finish(TruncateArgs a, int pieces, 
     some[i] = t >= rb.last_z && t > -INFINITY;
     if (some[i]) v[i].load(z_row, x0 + 1024 * i, V);
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int x = x0 + 1024 * i;
-    if (x - 4 * lane >= V) break;
+  // (A loop: unrolled, this kernel is 15 KB instead of 4, and a call's kernels, 57 KB, then do not stay in the cache of instructions: up to 2.5 us a launch.)
+#pragma unroll 1
+  for (int x = x0; x < x0 + 4096 && x - 4 * lane < V; x += 1024) {
     float y[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    u64 w = 0;
-    if (some[i]) {
+    Sum w{0, 0};
+    if (some[0]) {
       float z[4];
-      v[i].numbers(x, V, z);
+      v[0].numbers(x, V, z);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if (rb.endless) z[e] = z[e] == INFINITY ? 0.f : -INFINITY;
         if (kept(z[e], x + e)) {
           const float d = z[e] - rb.zero;
           y[e] = d > -INFINITY ? d / rb.temp : (float)(((double)z[e] - rb.zero) / rb.temp);  // (the difference alone may leave fp32)
-          if (add) w += wt.number(z[e]);
+          if (add) w = w + wt.number(z[e]);
         }
       }
     }
+#pragma unroll
+    for (int i = 0; i < 3; ++i) { v[i] = v[i + 1]; some[i] = some[i + 1]; }
     if (add) {
-      if (__any(w != 0)) w = sum_to_lane(w);
+      if (__any((w.lo | w.hi) != 0)) w = sum_to_lane(w);
       if (lane == 63) a.sums[(int64_t)row * a.stretches + (x >> 8)] = w;
     }
     if (write) {
@@ -864,7 +959,8 @@ __global__ __launch_bounds__(256) void k_row_draw(TruncateArgs a) {
   const RowBorder rb = a.border[row];
   if (rb.drawn) return;
   const RowScale sc(a, row, rb.temp);
-  draw_token<T, VEC, 256>(sh, a, row, sc, Kept{rb.last_z, rb.last_id}, a.sums + (int64_t)row * a.stretches, a.stretches, 1);
+  const Sum *sums = a.sums + (int64_t)row * a.stretches;
+  draw_token<T, VEC, 256>(sh, a, row, sc, Kept{rb.last_z, rb.last_id}, [&](int i) { return sums[i]; }, a.stretches, 1);
 }
 
 }  // namespace spec
