@@ -1,10 +1,13 @@
-"""spec_truncate_logits where its sums have most to add up: one likely token before a tail of equal, unlikely ones, with vocabularies up to millions of tokens.
-The tail's weights are all off in the same direction, so that their errors add up."""
+"""spec_truncate_logits over large vocabularies.  Where its sums have most to add up: one likely token before a tail of equal, unlikely ones, whose weights are all off
+in the same direction, so that their errors add up.  And every rule and the draw's ends where a piece of the row's maxima is more than 4096 tokens and a
+stretch of a draw from the list more than 256, which they are above 262144."""
 import math
 
 import numpy as np
 import pytest
 import torch
+
+from test_gpu_truncate import check, logits_of, rules_of
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -65,3 +68,18 @@ def test_a_vocabulary_of_millions(B):
     one_peak(B, 1 << 24, -26.7, 0.99999, torch.float32, (1 << 24) - 1, 1e-5)
     one_peak(B, 1 << 26, -25.0, 0.9999, torch.bfloat16, 5, 0.9999)
     one_peak(B, 1 << 28, -24.4, 0.999, torch.bfloat16, 1 << 20, 0.9)
+
+
+@pytest.mark.parametrize("td", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [151936, 300001, 600000, 1000003])
+def test_rules_and_draws_over_large_vocabularies(B, V, td):
+    z = logits_of(5, 1, V, td, seed=V)
+    z[4, 0, V - 3:] = 40.0  # the last tokens, and none else to speak of
+    z[4, 0, 300:700] = 12.0
+    rules, on = rules_of(B, temperature=[1.0, 0.8, 1.2, 1.0, 1.0], top_k=[50, 5000, 0, 700, 350], top_p=[1.0, 1.0, 0.9, 0.7, 1.0], min_p=[0.0, 0.0, 0.0, 1e-3, 0.0])
+    for u in (0.0, 0.3, 0.5, 0.8, 1 - 2.0 ** -24):
+        us = torch.full((5, 1), u)
+        out, tokens = B.spec_truncate_logits(z, rules, uniforms=us.to(DEV))
+        check(z, out, on["temperature"], on["top_k"], on["top_p"], on["min_p"], us, tokens.cpu())
+        alone = B.spec_truncate_logits(z, rules, uniforms=us.to(DEV), want_logits=False)[1]
+        assert torch.equal(alone, tokens)
