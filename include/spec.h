@@ -509,7 +509,8 @@ int spec_paged_append_normed(void *hip_stream, const spec_paged_cache *cache, co
    values likewise.  Strides in bytes, multiples of 16; d_k and d_v 16-byte aligned, the scales 8-byte aligned.  Sizes and limits otherwise as of
    spec_paged_cache; dtype is that of the row-wise tensors, SPEC_DTYPE_BF16 or SPEC_DTYPE_F16 (SPEC_ERR_UNSUPPORTED for fp32).
    Half the bytes of a cache of 16 bits and one more a head: nearly twice the positions in the same memory, and attention of few rows in 0.6 of the time.
-   An element is off by at most 1 / 16 of itself, or 2^-10 of its scale where that is more (2^-18 of the head's largest).  */
+   An element is off by at most 1 / 16 of itself, or 2^-10 of its scale where that is more: 2^-17.8 of the head's largest, or 2^-25 (fp16) or 2^-110 (bf16)
+   where the scale is the least that spec_paged8_append gives.  */
 typedef struct {
   int32_t dtype;
   int32_t head_dim, n_kv_heads, page_size, n_pages;

@@ -13,7 +13,7 @@ struct e4m3_t { uint8_t v; };
 
 // What limits the scales of a cache for rows of type T.
 //   least   the least exponent: fp16's smallest number is 2^-24, the smallest code 2^-9; for bf16 far above the edge of its range
-//   most    the largest number of four bits that the type holds: larger magnitudes become it (off by 1 / 15.9 at most, within half a step of e4m3)
+//   most    the largest number of four bits that the type holds: larger magnitudes become it (off by less than 1 / 16 of themselves, as any code may be)
 //   beyond  from here on a magnitude rounds to the type's infinity
 template <class T> struct Codes;
 template <> struct Codes<bf16_t> {
