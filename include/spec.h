@@ -398,7 +398,7 @@ typedef struct {
 } spec_sampling_rules;
 
 /* spec_truncate_logits: the rules on d_logits, [B][s+1] rows as of spec_process_logits (any type, padded).
-     d_out [B][s+1][vocab] fp32 or NULL: x of the tokens that are kept (-infinity where it leaves fp32), -infinity for the others: what spec_sample_accept and spec_sample_tokens take with
+     d_out [B][s+1][vocab] fp32 or NULL: x of the tokens that are kept, rounded once (-infinity where it leaves fp32), -infinity for the others: what spec_sample_accept and spec_sample_tokens take with
      temperature 1 (target and draft rows alike), and what the round's acceptance is then exact for.  May be d_logits itself where the type
      is fp32 and row_stride = vocab.
      d_tokens [B][s+1] or NULL (not both): a draw from the kept tokens with d_uniforms [B][s+1], numbers in [0, 1): the lowest id whose cumulative weight

@@ -902,6 +902,7 @@ __global__ __launch_bounds__(256) void k_row_finish(TruncateArgs a, int pieces, 
   const RowBorder rb = a.border[row];
   const Kept kept{rb.last_z, rb.last_id};
   const Weights wt{(double)rb.zero, rb.c, a.shift};
+  const double per_temp = 1. / (double)rb.temp;
   add = add && !rb.drawn;
   if (!write && !add) return;
   const int x0 = piece * 4096 + 4 * threadIdx.x;
@@ -928,8 +929,7 @@ __global__ __launch_bounds__(256) void k_row_finish(TruncateArgs a, int pieces, 
       for (int e = 0; e < 4; ++e) {
         if (rb.endless) z[e] = z[e] == INFINITY ? 0.f : -INFINITY;
         if (kept(z[e], x + e)) {
-          const float d = z[e] - rb.zero;
-          y[e] = d > -INFINITY ? d / rb.temp : (float)(((double)z[e] - rb.zero) / rb.temp);  // (the difference alone may leave fp32)
+          y[e] = (float)(((double)z[e] - rb.zero) * per_temp);  // (rounded once; the difference alone may leave fp32)
           if (add) w = w + wt.number(z[e]);
         }
       }
