@@ -152,3 +152,30 @@ def test_the_largest_tiles_first_call_may_be_captured():
     tests = os.path.dirname(os.path.abspath(__file__))
     r = subprocess.run([sys.executable, "-c", FIRST_CALL, os.path.dirname(tests), tests], capture_output=True, text=True, timeout=110)
     assert r.returncode == 0 and "replays agree" in r.stdout, r.stderr[-3000:]
+
+
+@pytest.mark.parametrize("td", TYPES)
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("Hq,Hk,rows,lens,window,kernels", [
+    (4, 2, [2, 1, 3], [700, 33, 90], 0, [("k_paged_attend", 1)]), (16, 1, [4, 2], [3001, 70], 1700, [("k_paged_attend", 4), ("k_paged_join_rows", 4)]),
+    (8, 2, [70, 33], [333, 1040], 200, [("k_paged_chunk", 4)]), (64, 16, [900, 1101], [1000, 1101], 300, [("k_paged_chunk", 8)])])
+def test_any_bytes_where_no_row_looks(B, td, hd, Hq, Hk, rows, lens, window, kernels):
+    """Pools as they come: any codes under any scale byte, those of infinity among them, in pages that nothing was written to and in front of the window."""
+    b = ref.Batch(rows, lens, 16, seed=hd + Hk, absent=((0, 1),))
+    c = Cache(b, Hk, hd, td)
+    seen = torch.zeros((b.n_pages, b.page), dtype=torch.bool)
+    for s in range(b.B):
+        for p in range(max(0, lens[s] - rows[s] - window + 1) if window else 0, lens[s]):
+            if 0 <= int(b.table[s, p // 16]) < b.n_pages:
+                seen[b.table[s, p // 16], p % 16] = True
+    want_k, want_v = c.numbers()
+    for part in range(2):
+        c.codes[part][~seen] = torch.randint(0, 256, c.codes[part][~seen].shape, generator=b.g).to(torch.uint8)
+        scales = c.scales[part].transpose(1, 2)
+        scales[~seen] = torch.randint(0, 256, scales[~seen].shape, generator=b.g).to(torch.uint8)
+        scales[~seen] = torch.where(torch.rand(scales[~seen].shape, generator=b.g) < 0.2, 255, scales[~seen].int()).to(torch.uint8)
+    q = b.heads(Hq, hd, td)
+    got = attend(B, b, c, q, window, [(k, [hd, n]) for k, n in kernels], max_len=max(lens))
+    n = b.row_start[-1]
+    want, err = ref.attention(want_k, want_v, b, q, hd ** -0.5, window)
+    close(got[:n], want[:n], err[:n], td)
