@@ -47,7 +47,7 @@ struct Sum {
   static constexpr u64 MASK = (1ull << LOW) - 1;
   u64 lo, hi;
   __device__ __forceinline__ Sum operator+(const Sum &o) const { return Sum{lo + o.lo, hi + o.hi}; }
-  __device__ __forceinline__ Sum operator-(const Sum &o) const { return Sum{lo - o.lo, hi - o.hi}; }  // (of a part of the same terms)
+  __device__ __forceinline__ Sum operator-(const Sum &o) const { return Sum{lo - o.lo, hi - o.hi}; }  // (only of a term that was added as it is: nothing is borrowed)
   __device__ __forceinline__ Sum plain() const { return Sum{lo & MASK, hi + (lo >> LOW)}; }
   __device__ __forceinline__ double about() const { return (double)hi * (MASK + 1) + (double)lo; }
   static __device__ __forceinline__ Sum whole(double v) {  // of one from 0 on, below 2^94
@@ -265,16 +265,19 @@ __device__ __forceinline__ bool find_bin(Truncate<NT> &sh, const uint32_t *cnt, 
   to_c += before_cnt; to_m = to_m + sh.before;
   const Sum target = sh.target;
   auto short_of = [&](uint32_t c, const Sum &m) { return by_mass ? less(m, target) : c < (uint32_t)target.lo; };
-  if (!short_of(to_c, to_m) && short_of(to_c - c, to_m - m)) {
-    // from the last of the thread's bins back to the one that reaches it
+  Sum at = to_m - m;
+  uint32_t at_c = to_c - c;
+  if (!short_of(to_c, to_m) && short_of(at_c, at)) {
+    // (sums only grow here: a bin taken off the sum of several may ask for a carry back)
 #pragma unroll 1
-    for (int i = first + PER - 1;; --i) {
-      const uint32_t own_c = cnt[i];
-      to_c -= own_c; to_m = to_m - masses(i, std::integral_constant<int, 1>());
-      if (short_of(to_c, to_m)) {
-        sh.found_bin = i; sh.found_cnt = to_c; sh.found_mass = to_m; sh.found_n = own_c;
+    for (int i = first; i < first + PER; ++i) {
+      const uint32_t next_c = at_c + cnt[i];
+      const Sum next = at + masses(i, std::integral_constant<int, 1>());
+      if (!short_of(next_c, next)) {
+        sh.found_bin = i; sh.found_cnt = at_c; sh.found_mass = at; sh.found_n = cnt[i];
         break;
       }
+      at_c = next_c; at = next;
     }
   }
   __syncthreads();

@@ -83,3 +83,15 @@ def test_rules_and_draws_over_large_vocabularies(B, V, td):
         check(z, out, on["temperature"], on["top_k"], on["top_p"], on["min_p"], us, tokens.cpu())
         alone = B.spec_truncate_logits(z, rules, uniforms=us.to(DEV), want_logits=False)[1]
         assert torch.equal(alone, tokens)
+
+
+@pytest.mark.parametrize("spread", [0.02, 0.05, 0.2, 0.7])
+@pytest.mark.parametrize("V", [300, 2000, 9001, 40000])
+def test_borders_among_the_likeliest_bins(B, V, spread):
+    """The border in one of the first bins of a sixty-fourth of an octave, with tokens in those beside it."""
+    g = torch.Generator().manual_seed(V)
+    z = -spread * torch.rand((24, 2, V), generator=g)
+    rules, on = rules_of(B, top_p=[(i + 1) / 25 for i in range(24)], top_k=[0, V - V // 3] * 12)
+    u = torch.rand((24, 2), generator=g)
+    out, tokens = B.spec_truncate_logits(z.to(DEV), rules, uniforms=u.to(DEV))
+    check(z, out, k=on["top_k"], p=on["top_p"], u=u, tokens=tokens.cpu())
