@@ -406,7 +406,8 @@ typedef struct {
      d_workspace: scratch of spec_truncate_logits_workspace_bytes(), 256-byte aligned; calls that may overlap need one each.
    Weights are computed in 64 bits (to 3e-13 of themselves) and rounded to 50 bits (62 - bits with vocabularies of more than 2^12 tokens, of up to 2^bits;
    those below 2^-32 of the largest to 2^(bits - 94) of it).  Their sums are exact and the same in whatever order: which tokens are kept and drawn differs from
-   the definition only where a sum lies within some 10^-12 (10^-10 with more than 2^22 tokens) of the whole sum from its limit.  Enqueues on hip_stream (NULL = the default stream), needs no context, does not wait.
+   the definition only where a sum lies within some 10^-12 (10^-10 with more than 2^22 tokens) of the whole sum from its limit.
+   Enqueues on hip_stream (NULL = the default stream), needs no context, does not wait.
    s <= 15, B <= 65535, vocab <= 2^28 (SPEC_ERR_CAPACITY). */
 int spec_truncate_logits_workspace_bytes(int32_t B, int32_t s, int32_t vocab, size_t *bytes);
 int spec_truncate_logits(void *hip_stream, const void *d_logits, int32_t dtype, int64_t row_stride, int32_t B, int32_t s, int32_t vocab,

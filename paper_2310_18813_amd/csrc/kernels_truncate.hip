@@ -18,8 +18,8 @@
 //                   its limit.  What the maxima rule out is not read.  Draws, where all that is kept is in the list.
 //   k_row_finish    the result; logits that the maxima rule out are not read.  Sums of the kept weights by 256 tokens, for
 //   k_row_draw      the other rows' draws.
-// 64 x 4 rows of 50272 bf16 logits, each sequence with its own rules: 9 + 14 + 33 + 16 + 4.6 us of 76; 24 x 8 fp32 rows of 151936: 28 + 15 + 44 + 28 + 5 of
-// 120; one row of 32000: 21, greedy 10.  The maxima and the result are at memory's rate (a copy's); the border is a chain of passes, 1.5 to 3 us
+// 64 x 4 rows of 50272 bf16 logits, each sequence with its own rules: 9 + 14 + 36 + 17 + 5 us of 80; 24 x 8 fp32 rows of 151936: 28 + 15 + 46 + 28 + 5 of
+// 124; one row of 32000: greedy 14, top-k 26, top-p of flat logits 44.  The maxima and the result are at memory's rate (a copy's); the border is a chain of passes, 1.5 to 3 us
 // each from the list, and of trips to L2 where it reads the row: a workgroup a row, those whose border lies among all tokens last.  A
 // workgroup for all of a row took 113, 297 and 45: rows that need all their weights kept their CU while others had nothing to do.
 // What cost most in LDS: additions that return a place in a list, all to one word (3000 of them 30 us), so that a wave counts its tokens first.
@@ -920,7 +920,7 @@ __global__ __launch_bounds__(256) void k_row_finish(TruncateArgs a, int pieces, 
     some[i] = t >= rb.last_z && t > -INFINITY;
     if (some[i]) v[i].load(z_row, x0 + 1024 * i, V);
   }
-  // (A loop: unrolled, this kernel is 15 KB instead of 4, and a call's kernels, 57 KB, then do not stay in the cache of instructions: up to 2.5 us a launch.)
+  // (A loop: unrolled, this kernel is 15 KB of instructions, not 4.)
 #pragma unroll 1
   for (int x = x0; x < x0 + 4096 && x - 4 * lane < V; x += 1024) {
     float y[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};

@@ -1041,6 +1041,7 @@ struct Shape {
 // where these make two rounds of workgroups and more.  us with 128 and with 256, bf16, 32 heads over 8: six sequences of 1000 rows (768 tiles of 256)
 // over up to 8192 positions 702 and 652 with heads of 128, 409 and 409 with heads of 64; one of 1500 (192 tiles) over 2048 positions
 // 68 and 66, 40 and 47; over 8192 253 and 219, 148 and 153.  So with few tiles heads of 64 gain from 128, heads of 128 would not need them.
+// (All figures here are of caches of 16 bits.  One of 8 goes by the same rules; its own sides were not measured.)
 static Shape attend_shape(const spec_paged_cache *c, const spec_paged_batch *b, int n_q, int window) {
   Shape s{};
   const int64_t Hk = c->n_kv_heads, G = n_q / Hk, per = (int64_t)b->max_rows * G;
