@@ -95,3 +95,16 @@ def test_borders_among_the_likeliest_bins(B, V, spread):
     u = torch.rand((24, 2), generator=g)
     out, tokens = B.spec_truncate_logits(z.to(DEV), rules, uniforms=u.to(DEV))
     check(z, out, k=on["top_k"], p=on["top_p"], u=u, tokens=tokens.cpu())
+
+
+def test_many_tokens_just_behind_the_border_s_bin(B):
+    """Large logits, whose differences are uncertain by more than a bin: what lies just behind the border's bin comes to the list with it."""
+    g = torch.Generator().manual_seed(31)
+    z = torch.full((24, 1, 9001), 1000.0)
+    d = torch.cat([0.1191 * torch.rand((24, 1, 80), generator=g), 0.11913 + 0.0009 * torch.rand((24, 1, 3000), generator=g)], -1)
+    at = torch.stack([torch.randperm(9001, generator=g)[:3080] for _ in range(24)])[:, None]
+    z.scatter_(-1, at, 1024.0 - d)
+    rules, on = rules_of(B, top_p=[0.001 + 0.0012 * i for i in range(24)], top_k=[0, 0, 3050] * 8)
+    u = torch.rand((24, 1), generator=g)
+    out, tokens = B.spec_truncate_logits(z.to(DEV), rules, uniforms=u.to(DEV))
+    check(z, out, k=on["top_k"], p=on["top_p"], u=u, tokens=tokens.cpu())
